@@ -476,10 +476,9 @@ pex_status pex_layer_norm_grad(const void *G, const void *X, const float *mean, 
  *   thousandths of |M|_F and more near 1.
  *   M, O [count, rows, cols]  device, dtype `dt`; O may be M.  A matrix of zeros stays zero, one that holds an infinity or a NaN is NaN
  *                   throughout; it does not touch the others.
- *   Products are exact to 2^-22 and summed in fp32 for fp32 matrices (O as close to the exact result as by fp32 products, or closer);
- *   for bf16 matrices the iterates are rounded to 11 bits (not of small ones and ones of at most 64 rows or columns), O is rounded to bf16
- *   once.  The norm is summed in fp64.  Entries of X
- *   below 2^-36 vanish: a matrix whose norm is far below eps comes out as zeros.
+ *   Products are exact to 2^-22 and summed in fp32, for either type (O as close to the exact result as by fp32 products, or closer); O of
+ *   bf16 matrices is rounded to bf16 once.  The norm is summed in fp64.  Entries of X below 2^-36 vanish: a matrix whose norm is far below
+ *   eps comes out as zeros.
  *   workspace       pex_orthogonalize_workspace_bytes(...) bytes, 16-byte aligned; one matrix's (the query for count = 1) is enough, the
  *                   matrices then go through it one after the other: the same bits.  (How products are divided, and with it the
  *                   last bits, goes by the sizes and number of the matrices of a call.)

@@ -1585,7 +1585,7 @@ static pex_status check_ns_params(const pex_newton_schulz_params& p)
 size_t pex_orthogonalize_workspace_bytes(int64_t count, int64_t rows, int64_t cols, pex_dtype dt)
 {
     if (count < 1 || count >= ((int64_t)1 << 31) || !ns_shape_ok(rows, cols) || (dt != PEX_F32 && dt != PEX_BF16)) return 0;
-    return (size_t)count * ns_matrix_bytes(rows, cols, dt);
+    return (size_t)count * ns_matrix_bytes(rows, cols);
 }
 
 pex_status pex_orthogonalize(const void* M, void* O, int64_t count, int64_t rows, int64_t cols, pex_dtype dt, const pex_newton_schulz_params* p,
@@ -1597,7 +1597,7 @@ pex_status pex_orthogonalize(const void* M, void* O, int64_t count, int64_t rows
     const pex_status st = check_ns_params(*p);
     if (st != PEX_OK) return st;
     if (((uintptr_t)M | (uintptr_t)O) & (dt == PEX_BF16 ? 1u : 3u)) return PEX_ERR_ALIGN;
-    if (!workspace || workspace_bytes < ns_matrix_bytes(rows, cols, dt)) return PEX_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < ns_matrix_bytes(rows, cols)) return PEX_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 15u) return PEX_ERR_ALIGN;
     const NsMatrix m = {const_cast<void*>(M), nullptr, O, rows, cols, count, 0.f};
     const NsCall call = {p->a, p->b, p->c, p->eps, p->steps, ns_coefficients(*p) == 2, 0.f, 0.f, 0.f, 0};
@@ -1610,7 +1610,7 @@ size_t pex_muon_step_workspace_bytes(const pex_muon_tensor* tensors, int32_t cou
     size_t need = 0;
     for (int k = 0; k < count; ++k) {
         if (!ns_shape_ok(tensors[k].rows, tensors[k].cols)) return 0;
-        need += ns_matrix_bytes(tensors[k].rows, tensors[k].cols, PEX_F32);
+        need += ns_matrix_bytes(tensors[k].rows, tensors[k].cols);
     }
     return need;
 }
@@ -1629,7 +1629,7 @@ pex_status pex_muon_step(const pex_muon_tensor* tensors, int32_t count, const pe
         if (!t.theta || !t.m || !t.S) return PEX_ERR_NULL;
         if (!ns_shape_ok(t.rows, t.cols)) return PEX_ERR_SHAPE;
         if (((uintptr_t)t.theta | (uintptr_t)t.m | (uintptr_t)t.S) & 3u) return PEX_ERR_ALIGN;
-        const size_t own = ns_matrix_bytes(t.rows, t.cols, PEX_F32);
+        const size_t own = ns_matrix_bytes(t.rows, t.cols);
         if (own > least) least = own;
     }
     if (!workspace || workspace_bytes < least) return PEX_ERR_WORKSPACE;

@@ -4,18 +4,17 @@
 // its transpose where it is taller than wide): s rows, l >= s columns.  Per step s^2 l + s^3 + 2 s^2 l operations: A and A^2 are
 // symmetric, half of their blocks are computed.
 //
-// Products on the fp16 matrix cores.  A bf16 matrix is held as one fp16 piece per value (11 bits, eight times as fine as bf16): against
-// 64 bits the result is off by 2.1e-3 of the 2-norm, its own rounding to bf16 alone is 1.66e-3 of that, bf16 pieces would
-// make it 1e-2.  An fp32 matrix is held as two pieces, x = hi + lo to 22 bits and more, and a product is hi hi + hi lo + lo hi (lo lo is
-// below 2^-22 of it): 3e-7 where fp32 products give 2e-6 to 1e-5 (their order of additions), at three products instead of one that
-// runs at a tenth of the rate.  Powers of two keep the pieces inside fp16's range: X by 2^12, A by 2^9, P by 2^10; the host
-// refuses coefficients under which singular values leave [0, 4] or P's leave [-31, 31].
+// Products on the fp16 matrix cores.  A value is held as two pieces, x = hi + lo to 22 bits and more, and a product is hi hi + hi lo + lo hi
+// (lo lo is below 2^-22 of it): off by 3e-7 of the 2-norm where fp32 products give 2e-6 to 1e-5 (their order of additions), at three products
+// instead of one that runs at a tenth of the rate.  bf16 matrices too: what their result is off by is then its own rounding, 1.66e-3.  As
+// one piece (11 bits) they take half of the time (12 of 768 x 768: 260 us instead of 460) and are off by 2.1e-3.  Powers of two keep
+// the pieces inside fp16's range: X by 2^12, A by 2^9, P by 2^10; the host refuses coefficients under which singular values leave [0, 4] or
+// P's leave [-31, 31].
 //
 // Layout: every operand lies in the order in which the matrix cores take it, fragments of 16 rows x 32 columns, 64 lanes x 8 values =
-// 1 KiB, lane (row % 16) + 16 * (column / 8 % 4).  Four fragments are a unit of 32 rows, fragment 2 r + x: rows 16 r .., piece x of 32
-// columns, or of one piece the columns 32 x .. of 64; units of the same rows follow each other.  So a fragment is one
-// direct-to-LDS load without any address arithmetic per lane, LDS reads are conflict-free, and no product needs a transposing
-// read: both operands of every product are rows (A and P are symmetric), which costs X a second copy by columns that the kernel
+// 1 KiB, lane (row % 16) + 16 * (column / 8 % 4).  Four fragments are a unit of 32 rows and columns, fragment 2 r + x: rows 16 r .., piece x;
+// units of the same rows follow each other.  So a fragment is one direct-to-LDS load without any address arithmetic per lane, LDS reads are
+// conflict-free, and no product needs a transposing read: both operands of every product are rows (A and P are symmetric), which costs X a second copy by columns that the kernel
 // that makes X writes beside the first.  Sides are padded with zeros to whole blocks; zeros stay zeros.
 // (16 x 16 x 32: these products are bound by power, and of nothing but them the chip sustains 1630 TFLOP/s on Gaussian fp16 values, of
 // 32 x 32 x 16 ones 1430.)
@@ -116,17 +115,14 @@ __device__ __forceinline__ int row_of(int g, int lane) { return 16 * (g >> 1) + 
 __device__ __forceinline__ int col_of(int g, int lane) { return 16 * (g & 1) + (lane & 15); }
 
 // fragment `x` (piece) of rows 16 r .. of unit (row, column) of an operand of `cols32` times 32 columns, in halves
-template <int PIECES>
 __device__ __forceinline__ int64_t fragment_at(int row32, int col32, int cols32, int r, int x)
 {
-    if (PIECES == 2) return (((int64_t)row32 * cols32 + col32) * 4 + 2 * r + x) * FRAG;
-    return (((int64_t)row32 * (cols32 / 2) + col32 / 2) * 4 + 2 * r + (col32 & 1)) * FRAG;
+    return (((int64_t)row32 * cols32 + col32) * 4 + 2 * r + x) * FRAG;
 }
 // where piece p of a quarter lies in C's transpose: half a lane's 16 bytes of a fragment
-template <int PIECES>
 __device__ __forceinline__ half4_t* place(char* base, int rows32, int i32, int j32, int g, int p, int lane)
 {
-    return (half4_t*)((_Float16*)base + fragment_at<PIECES>(j32, i32, rows32, g & 1, p) + ((lane & 15) + 16 * (2 * (g >> 1) + (lane >> 5))) * 8 + 4 * (lane >> 4 & 1));
+    return (half4_t*)((_Float16*)base + fragment_at(j32, i32, rows32, g & 1, p) + ((lane & 15) + 16 * (2 * (g >> 1) + (lane >> 5))) * 8 + 4 * (lane >> 4 & 1));
 }
 
 // the result itself: quarters [from, to) of a tile
@@ -155,7 +151,6 @@ __device__ __forceinline__ void put_out(const Jobs& jobs, const Job& j, int copy
 }
 
 // The entries of C as pieces, written by columns; hi | lo << 16 of the four come back for the copy by rows
-template <int PIECES>
 __device__ __forceinline__ void put_by_cols(const Job& j, int64_t at, int i32, int j32, int g, float4_t x, uint32_t (&packed)[4], int lane)
 {
 #pragma unroll
@@ -165,8 +160,7 @@ __device__ __forceinline__ void put_by_cols(const Job& j, int64_t at, int i32, i
     }
     auto add = [&](const _Float16* from, float times) {
         char* base = (char*)from + at;
-        half4_t hi = *place<PIECES>(base, j.m32, i32, j32, g, 0, lane), lo = {};
-        if (PIECES == 2) lo = *place<PIECES>(base, j.m32, i32, j32, g, 1, lane);
+        const half4_t hi = *place(base, j.m32, i32, j32, g, 0, lane), lo = *place(base, j.m32, i32, j32, g, 1, lane);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = fmaf(times, (float)hi[e] + (float)lo[e], x[e]);
     };
@@ -182,8 +176,8 @@ __device__ __forceinline__ void put_by_cols(const Job& j, int64_t at, int i32, i
         packed[e] = (uint32_t)__builtin_bit_cast(uint16_t, a) | (uint32_t)__builtin_bit_cast(uint16_t, b) << 16;
     }
     char* to = (char*)j.by_cols + at;
-    *place<PIECES>(to, j.m32, i32, j32, g, 0, lane) = hi;
-    if (PIECES == 2) *place<PIECES>(to, j.m32, i32, j32, g, 1, lane) = lo;
+    *place(to, j.m32, i32, j32, g, 0, lane) = hi;
+    *place(to, j.m32, i32, j32, g, 1, lane) = lo;
 }
 
 constexpr int TURN = 32 * 32;        // dwords of LDS in which a tile is turned; column c of row r lies at c ^ r: different banks both ways
@@ -196,7 +190,6 @@ __device__ __forceinline__ void turn_in(uint32_t* turn, int g, const uint32_t (&
     }
 }
 // rows 16 r .. of a turned tile
-template <int PIECES>
 __device__ __forceinline__ void put_by_rows(const Job& j, int64_t at, int i32, int j32, int r, const uint32_t* turn, int lane)
 {
     const int row = 16 * r + (lane & 15);
@@ -210,12 +203,12 @@ __device__ __forceinline__ void put_by_rows(const Job& j, int64_t at, int i32, i
         piece[1][e] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xffff0000u);
     }
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p)
-        *(uint4_t*)((_Float16*)((char*)j.by_rows + at) + fragment_at<PIECES>(i32, j32, j.n32, r, p) + lane * 8) = piece[p];
+    for (int p = 0; p < 2; ++p)
+        *(uint4_t*)((_Float16*)((char*)j.by_rows + at) + fragment_at(i32, j32, j.n32, r, p) + lane * 8) = piece[p];
 }
 
 // a whole tile by one wave; `turn` is its own
-template <int PIECES, typename TOut, bool UPDATE>
+template <typename TOut, bool UPDATE>
 __device__ __forceinline__ void put_tile(const Jobs& jobs, const Job& j, const Block& b, int64_t at, int i32, int j32, const Tile& x, uint32_t* turn, int lane)
 {
     if (j.out) {
@@ -225,34 +218,26 @@ __device__ __forceinline__ void put_tile(const Jobs& jobs, const Job& j, const B
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
         uint32_t packed[4];
-        put_by_cols<PIECES>(j, at, i32, j32, g, x.q[g], packed, lane);
+        put_by_cols(j, at, i32, j32, g, x.q[g], packed, lane);
         turn_in(turn, g, packed, lane);
     }
     if (j.symmetric && b.bi == b.bj) return;     // a block on the diagonal is its own transpose
     __builtin_amdgcn_wave_barrier();
-    put_by_rows<PIECES>(j, at, i32, j32, 0, turn, lane);
-    put_by_rows<PIECES>(j, at, i32, j32, 1, turn, lane);
+    put_by_rows(j, at, i32, j32, 0, turn, lane);
+    put_by_rows(j, at, i32, j32, 1, turn, lane);
     __builtin_amdgcn_wave_barrier();
 }
 
-// The products of one tile and one unit of columns.  Two pieces: from zero, the small ones first; their sum is added to the tile by vector
+// The products of one tile and one unit of columns: from zero, the small ones first; their sum is added to the tile by vector
 // instructions, which round to nearest (the matrix cores do not, and a long chain of them drifts).
-template <int PIECES>
 __device__ __forceinline__ void products(const half8_t (&u)[4], const half8_t (&v)[4], Tile& d)
 {
-    if constexpr (PIECES == 2) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) d.q[g] = mfma(u[(g & 2) + 1], v[2 * (g & 1)], float4_t{0.f, 0.f, 0.f, 0.f});
+    for (int g = 0; g < 4; ++g) d.q[g] = mfma(u[(g & 2) + 1], v[2 * (g & 1)], float4_t{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-        for (int g = 0; g < 4; ++g) d.q[g] = mfma(u[g & 2], v[2 * (g & 1) + 1], d.q[g]);
+    for (int g = 0; g < 4; ++g) d.q[g] = mfma(u[g & 2], v[2 * (g & 1) + 1], d.q[g]);
 #pragma unroll
-        for (int g = 0; g < 4; ++g) d.q[g] = mfma(u[g & 2], v[2 * (g & 1)], d.q[g]);
-    } else {
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) d.q[g] = mfma(u[(g & 2) + x], v[2 * (g & 1) + x], d.q[g]);
-    }
+    for (int g = 0; g < 4; ++g) d.q[g] = mfma(u[g & 2], v[2 * (g & 1)], d.q[g]);
 }
 __device__ __forceinline__ void clear(Tile& t)
 {
@@ -268,7 +253,7 @@ __device__ __forceinline__ void add(Tile& t, const Tile& d)
 // ---- few blocks: operands straight from the caches to registers, four waves of a workgroup divide the columns of U and V among them.
 // No barrier in the loop and a load ahead: bound by the latency of the caches, then by what a compute unit takes from its L2.  Symmetric
 // 1024 x 1024 x 1024 of fp32 in 12.5 us, 512 x 512 x 512 in 6.
-template <int F, int PIECES, typename TOut, bool UPDATE>
+template <int F, typename TOut, bool UPDATE>
 __global__ __launch_bounds__(256) void ns_direct_kernel(Jobs jobs)
 {
     constexpr int WAVES = 4;
@@ -312,11 +297,9 @@ __global__ __launch_bounds__(256) void ns_direct_kernel(Jobs jobs)
         for (int m = 0; m < F; ++m)
 #pragma unroll
             for (int n = 0; n < F; ++n) {
-                if constexpr (PIECES == 2) {
-                    Tile d;
-                    products<2>(cu[m], cv[n], d);
-                    add(acc[m][n], d);
-                } else products<1>(cu[m], cv[n], acc[m][n]);
+                Tile d;
+                products(cu[m], cv[n], d);
+                add(acc[m][n], d);
             }
     }
     // the waves' sums, in their order
@@ -342,17 +325,17 @@ __global__ __launch_bounds__(256) void ns_direct_kernel(Jobs jobs)
             return;
         }
         uint32_t packed[4];
-        put_by_cols<PIECES>(j, at, b.bi, b.bj, wave, sum(0, wave), packed, lane);
+        put_by_cols(j, at, b.bi, b.bj, wave, sum(0, wave), packed, lane);
         if (j.symmetric && b.bi == b.bj) return;
         turn_in(turned, wave, packed, lane);
         __syncthreads();
-        if (wave < 2) put_by_rows<PIECES>(j, at, b.bi, b.bj, wave, turned, lane);
+        if (wave < 2) put_by_rows(j, at, b.bi, b.bj, wave, turned, lane);
     } else {                                // a tile
         Tile x;
 #pragma unroll
         for (int g = 0; g < 4; ++g) x.q[g] = sum(wave, g);
         __builtin_amdgcn_wave_barrier();
-        put_tile<PIECES, TOut, UPDATE>(jobs, j, b, at, b.bi * F + wave / F, b.bj * F + wave % F, x,
+        put_tile<TOut, UPDATE>(jobs, j, b, at, b.bi * F + wave / F, b.bj * F + wave % F, x,
                                        (uint32_t*)(sums + wave * 256), lane);       // (what wave 0 left of this tile; nobody else reads it)
     }
 }
@@ -361,7 +344,7 @@ __global__ __launch_bounds__(256) void ns_direct_kernel(Jobs jobs)
 // row fragments and streams the column fragments: those of the next tiles are read under the products of the present ones, across
 // the one barrier a slot has (before the products with the last column fragment: by then the wave has read all of the slot, and all of the
 // next one has arrived).  Blocks of 256 x 256 (128 KiB of LDS) or, two workgroups to a compute unit, 128 x 128; where there are no two
-// workgroups for each, four slots for one: loads are on their way for longer (bf16 2816 x 2816, 253 blocks: 643 -> 565 us a call).
+// workgroups for each, four slots for one: loads are on their way for longer.
 // Measured, two matrices, 2048 x 8192 = (2048 x 2048) (2048 x 8192): 256 346 us = 1193 TFLOP/s of fp16 products, 128 394 (1047), the kernel
 // above with 64 612 (673); 272 blocks of 128 of a symmetric 2048 x 2048 x 8192 250 us, in blocks of 256 455, of 64 316.
 __device__ __forceinline__ void dma_16_at(uint32_t lds_addr, uint32_t voff, uint32_t soff, int4_t rsrc)
@@ -374,7 +357,7 @@ template <int B> constexpr int slot_bytes() { return 2 * B / 32 * 4096; }
 // DIVIDED (symmetric products): some blocks are divided along their columns, one part a workgroup; the parts go to memory, and who comes last
 // adds them up, in their order: nobody waits.  All parts of one range of columns are next to each other, so that their workgroups share
 // panels in the L2 (every workgroup its own range: two of 2048 x 8192 took 16 % more time instead of 5 % less).
-template <int B, int PIECES, typename TOut, bool UPDATE, bool DIVIDED, int SLOTS = 2>
+template <int B, typename TOut, bool UPDATE, bool DIVIDED, int SLOTS = 2>
 __global__ __launch_bounds__(512, B == 256 || SLOTS > 2 ? 2 : 4) void ns_staged_kernel(Jobs jobs)
 {
     constexpr int WM = 4, WN = 2, FM = B / WM / 32, FN = B / WN / 32, SLOT = slot_bytes<B>(), LOADS = SLOT / 1024 / 8;
@@ -467,17 +450,15 @@ __global__ __launch_bounds__(512, B == 256 || SLOTS > 2 ? 2 : 4) void ns_staged_
 #pragma unroll
             for (int m = 0; m < FM; ++m) {
                 const int t = n * FM + m;
-                if constexpr (PIECES == 2) {
-                    products<2>(u[m], v[n & 1], d[t & 1]);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (t > 0) add(acc[(t - 1) % FM][(t - 1) / FM], d[(t - 1) & 1]);
-                } else products<1>(u[m], v[n & 1], acc[m][n]);
+                products(u[m], v[n & 1], d[t & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (t > 0) add(acc[(t - 1) % FM][(t - 1) / FM], d[(t - 1) & 1]);
                 if (n == FN - 1) read_u(m, next);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
         issue(s + SLOTS, slot);
-        if constexpr (PIECES == 2) add(acc[FM - 1][FN - 1], d[(FM * FN - 1) & 1]);
+        add(acc[FM - 1][FN - 1], d[(FM * FN - 1) & 1]);
     }
     wait_vmcnt<0>();
     wait_lds_and_barrier();                    // the slots are free
@@ -524,7 +505,7 @@ __global__ __launch_bounds__(512, B == 256 || SLOTS > 2 ? 2 : 4) void ns_staged_
     for (int m = 0; m < FM; ++m)
 #pragma unroll
         for (int n = 0; n < FN; ++n)
-            put_tile<PIECES, TOut, UPDATE>(jobs, j, b, at, b.bi * (B / 32) + wm * FM + m, b.bj * (B / 32) + wn * FN + n, acc[m][n], turn, lane);
+            put_tile<TOut, UPDATE>(jobs, j, b, at, b.bi * (B / 32) + wm * FM + m, b.bj * (B / 32) + wn * FN + n, acc[m][n], turn, lane);
 }
 
 // ---- before the products: the norm, and X_0 as operands --------------------------------------------------------------
@@ -628,7 +609,7 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(Sources src)
 }
 
 // A 64 x 64 tile of X_0: by rows and by columns
-template <typename T, int PIECES, bool UPDATE>
+template <typename T, bool UPDATE>
 __global__ __launch_bounds__(256) void ns_prepare_kernel(Sources src)
 {
     __shared__ float tile[64][65];
@@ -677,18 +658,17 @@ __global__ __launch_bounds__(256) void ns_prepare_kernel(Sources src)
         }
         _Float16* to = (_Float16*)((char*)(cols ? m.by_cols : m.by_rows) + (int64_t)copy * m.stride);
         const int row32 = (cols ? tj : ti) * 2 + (a16 >> 1), col32 = (cols ? ti : tj) * 2 + b32, cols32 = (cols ? m.s_tiles : m.l_tiles) * 2;
-        *((half8_t*)(to + fragment_at<PIECES>(row32, col32, cols32, a16 & 1, 0)) + lane) = hi;
-        if (PIECES == 2) *((half8_t*)(to + fragment_at<PIECES>(row32, col32, cols32, a16 & 1, 1)) + lane) = lo;
+        *((half8_t*)(to + fragment_at(row32, col32, cols32, a16 & 1, 0)) + lane) = hi;
+        *((half8_t*)(to + fragment_at(row32, col32, cols32, a16 & 1, 1)) + lane) = lo;
     }
 }
 
 // ---- small matrices: everything in one workgroup ---------------------------------------------------------------------
 //
-// A matrix of at most 64 KiB in pieces of fp32 (64 x 256, 128 x 128; padded to multiples of 64) stays in the LDS of one compute unit from
+// A matrix of at most 64 KiB in pieces (64 x 256, 128 x 128; padded to multiples of 64) stays in the LDS of one compute unit from
 // its norm to the result: X by rows, then A, then P in one half, X by columns in the other; the tiles of a product (at most sixteen, two a
 // wave) are in registers until everyone has read what they replace.  One launch where the kernels above take two and three a step, each of
-// which costs 4 us whatever it does (64 x 64: 72 -> 27 us for fifteen products one after the other).  Two pieces for bf16 matrices as
-// well: time is latency here.
+// which costs 4 us whatever it does (64 x 64: 72 -> 27 us for fifteen products one after the other).
 constexpr int SMALL_MOST = 16384;        // padded entries
 constexpr int SMALL_WAVES = 8, SMALL_TILES = SMALL_MOST / 1024 / SMALL_WAVES;
 
@@ -738,7 +718,7 @@ __global__ __launch_bounds__(SMALL_WAVES * 64) void ns_small_kernel(SmallJobs jo
     const double inv = (double)SCALE_X / (sqrt(ssq) + (double)jobs.eps);
     // entry (row, col) of an operand of cols32 times 32 columns
     auto put = [&](_Float16* to, int row, int col, int cols32, _Float16 hi, _Float16 lo) {
-        _Float16* p = to + fragment_at<2>(row >> 5, col >> 5, cols32, row >> 4 & 1, 0) + ((row & 15) + 16 * (col >> 3 & 3)) * 8 + (col & 7);
+        _Float16* p = to + fragment_at(row >> 5, col >> 5, cols32, row >> 4 & 1, 0) + ((row & 15) + 16 * (col >> 3 & 3)) * 8 + (col & 7);
         p[0] = hi;
         p[FRAG] = lo;
     };
@@ -773,7 +753,7 @@ __global__ __launch_bounds__(SMALL_WAVES * 64) void ns_small_kernel(SmallJobs jo
                     fv[f] = pv[s * 256 + f * 64];
                 }
                 Tile d;
-                products<2>(fu, fv, d);
+                products(fu, fv, d);
                 add(x[i], d);
             }
         }
@@ -804,8 +784,8 @@ __global__ __launch_bounds__(SMALL_WAVES * 64) void ns_small_kernel(SmallJobs jo
                     lo[e] = b;
                     if (!diagonal) put(by_rows, ti * 32 + row_of(g, lane) + e, tj * 32 + col_of(g, lane), rows_cols32, a, b);
                 }
-                *place<2>((char*)by_cols, cols_cols32, ti, tj, g, 0, lane) = hi;
-                *place<2>((char*)by_cols, cols_cols32, ti, tj, g, 1, lane) = lo;
+                *place((char*)by_cols, cols_cols32, ti, tj, g, 0, lane) = hi;
+                *place((char*)by_cols, cols_cols32, ti, tj, g, 1, lane) = lo;
             }
         }
     };
@@ -901,10 +881,10 @@ struct ThinJobs {
     ThinJob job[THIN_JOBS];
 };
 
-// entry (row, col) of an operand of cols32 times 32 columns in two pieces
+// entry (row, col) of an operand of cols32 times 32 columns
 __device__ __forceinline__ _Float16* entry_at(_Float16* to, int row, int col, int cols32)
 {
-    return to + fragment_at<2>(row >> 5, col >> 5, cols32, row >> 4 & 1, 0) + ((row & 15) + 16 * (col >> 3 & 3)) * 8 + (col & 7);
+    return to + fragment_at(row >> 5, col >> 5, cols32, row >> 4 & 1, 0) + ((row & 15) + 16 * (col >> 3 & 3)) * 8 + (col & 7);
 }
 __device__ __forceinline__ void put_entry(_Float16* to, int row, int col, int cols32, float v)
 {
@@ -971,8 +951,8 @@ __global__ __launch_bounds__(512) void ns_thin_kernel(ThinJobs jobs)
                 hi[e] = p[0];
                 lo[e] = p[FRAG];
             }
-            *((half8_t*)(X + fragment_at<2>(j32, i32, THIN_S / 32, r16, 0)) + lane) = hi;
-            *((half8_t*)(X + fragment_at<2>(j32, i32, THIN_S / 32, r16, 1)) + lane) = lo;
+            *((half8_t*)(X + fragment_at(j32, i32, THIN_S / 32, r16, 0)) + lane) = hi;
+            *((half8_t*)(X + fragment_at(j32, i32, THIN_S / 32, r16, 1)) + lane) = lo;
         }
     } else {
         // the wave's 32 columns of X: on their way while A and P are made
@@ -1012,13 +992,13 @@ __global__ __launch_bounds__(512) void ns_thin_kernel(ThinJobs jobs)
                     fv[f] = ((const half8_t*)A)[((tj * (THIN_S / 32) + s) * 4 + f) * 64 + lane];
                 }
                 Tile d;
-                products<2>(fu, fv, d);
+                products(fu, fv, d);
                 add(x, d);
             }
             const float ka = jobs.a * SCALE_P, kb = jobs.b * (SCALE_P / SCALE_A), kc = jobs.c * (SCALE_P / (SCALE_A * SCALE_A));
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const half4_t hi = *place<2>((char*)A, THIN_S / 32, ti, tj, g, 0, lane), lo = *place<2>((char*)A, THIN_S / 32, ti, tj, g, 1, lane);
+                const half4_t hi = *place((char*)A, THIN_S / 32, ti, tj, g, 0, lane), lo = *place((char*)A, THIN_S / 32, ti, tj, g, 1, lane);
                 float4_t y;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -1040,7 +1020,7 @@ __global__ __launch_bounds__(512) void ns_thin_kernel(ThinJobs jobs)
 #pragma unroll
                     for (int f = 0; f < 4; ++f) fu[f] = ((const half8_t*)P)[((i32 * (THIN_S / 32) + s) * 4 + f) * 64 + lane];
                     Tile d;
-                    products<2>(fu, v[s], d);
+                    products(fu, v[s], d);
                     add(x, d);
                 }
 #pragma unroll
@@ -1066,8 +1046,8 @@ __global__ __launch_bounds__(512) void ns_thin_kernel(ThinJobs jobs)
                             lo[e] = p[FRAG] = b;
                         }
                         // over what this wave, and nobody else, has read
-                        *place<2>((char*)X, THIN_S / 32, i32, wave, g, 0, lane) = hi;
-                        *place<2>((char*)X, THIN_S / 32, i32, wave, g, 1, lane) = lo;
+                        *place((char*)X, THIN_S / 32, i32, wave, g, 0, lane) = hi;
+                        *place((char*)X, THIN_S / 32, i32, wave, g, 1, lane) = lo;
                     }
                 }
             }
@@ -1088,7 +1068,7 @@ __global__ __launch_bounds__(512) void ns_thin_kernel(ThinJobs jobs)
                     fv[f] = ((const half8_t*)rows_of_x)[((tj * (THIN_SLAB / 32) + s) * 4 + f) * 64 + lane];
                 }
                 Tile d;
-                products<2>(fu, fv, d);
+                products(fu, fv, d);
                 add(x, d);
             }
             float4_t* share = (float4_t*)((char*)j.share[FIRST ? 0 : 1] + at) + (int64_t)slab * THIN_SHARE + wave * 256 + lane;
@@ -1103,11 +1083,10 @@ __global__ __launch_bounds__(512) void ns_thin_kernel(ThinJobs jobs)
 int64_t padded(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // A side as the kernels see it: whole blocks of the largest kind that costs little padding.  Products go by the cube of it.  Whole calls (us),
 // 256 for up to an eighth more / a thirty-second: fp32 1100 x 1100 343 / 259, 3136 x 2488 1500 / 1248, 3400 x 3400 2718 / 2368, 2700 x 2700
-// 1294 / 1308; 128 always / for up to a ninth more than 64: fp32 10 of 1056 x 576 450 / 403, 16 of 192 x 768 156 / 134, bf16 12 of 448 x
-// 448 156 / 140, but 30 of 576 x 1024 459 / 510: with one piece the kernels that need 128 are the faster ones sooner.
-int64_t padded_side(int64_t n, int pieces)
+// 1294 / 1308; 128 always / for up to a ninth more than 64: 10 of 1056 x 576 450 / 403, 16 of 192 x 768 156 / 134.
+int64_t padded_side(int64_t n)
 {
-    if (n <= 64 || ((pieces == 2 || n <= 448) && padded(n, 64) * 10 <= padded(n, 128) * 9)) return padded(n, 64);
+    if (n <= 64 || padded(n, 64) * 10 <= padded(n, 128) * 9) return padded(n, 64);
     return padded(n, 256) * 32 <= padded(n, 128) * 33 ? padded(n, 256) : padded(n, 128);
 }
 
@@ -1120,21 +1099,20 @@ struct Layout {
     int parts;
     int64_t at[BUF_COUNT], partial_at, arrived_at, blocks, bytes;      // blocks: of 128 x 128 of a symmetric product
 };
-// Whether two steps at a time go through the Gram matrix (see program_of): where products bound the time and there are fewer of them so.  Not
-// with one piece (its roundings would grow too large).
-bool by_gram(int64_t s, int64_t l, int pieces) { return pieces == 2 && s >= 512 && 2 * l >= 3 * s; }
+// Whether two steps at a time go through the Gram matrix (see program_of): where products bound the time and there are fewer of them so
+bool by_gram(int64_t s, int64_t l) { return s >= 512 && 2 * l >= 3 * s; }
 
-Layout layout_of(int64_t rows, int64_t cols, int pieces)
+Layout layout_of(int64_t rows, int64_t cols)
 {
     Layout w{};
-    w.s = padded_side(rows < cols ? rows : cols, pieces);
-    w.l = padded_side(rows < cols ? cols : rows, pieces);
+    w.s = padded_side(rows < cols ? rows : cols);
+    w.l = padded_side(rows < cols ? cols : rows);
     const int64_t parts = (rows * cols + 2047) / 2048;
     w.parts = (int)(parts < MOST_PARTS ? parts : MOST_PARTS);
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t here = at; at += padded(bytes, 256); return here; };
-    for (int k = 0; k < (by_gram(w.s, w.l, pieces) ? BUF_COUNT : BUF_P1); ++k)      // step by step: A and one P
-        w.at[k] = take((k <= BUF_COLS1 ? w.s * w.l : w.s * w.s) * 2 * pieces);
+    for (int k = 0; k < (by_gram(w.s, w.l) ? BUF_COUNT : BUF_P1); ++k)      // step by step: A and one P
+        w.at[k] = take((k <= BUF_COLS1 ? w.s * w.l : w.s * w.s) * 4);
     w.partial_at = take((int64_t)w.parts * 8);
     w.blocks = w.s / 128 * (w.s / 128 + 1) / 2;
     w.arrived_at = take(w.blocks * 4);
@@ -1159,7 +1137,7 @@ struct Program {
 // With l = 4 s five steps as 2 + 2 + 1 are 47 s^3 products of two matrices instead of 65, three more launches.  Half of a product is taken for
 // the whole: the identity's share stays outside of it, where rounding would move the small eigenvalues of A by 2^-23 of the largest,
 // which a step lets grow by a^2 = 12.  Off by 1.1e-6 of the 2-norm (64 bits; 250 x 1002), step by step 4e-7, 3 + 2 steps 2.6e-6.
-void program_of(const Layout& w, int pieces, const NsCall& call, Program& p)
+void program_of(const Layout& w, const NsCall& call, Program& p)
 {
     p.count = 0;
     const float a = call.a, b = call.b, c = call.c;
@@ -1172,7 +1150,7 @@ void program_of(const Layout& w, int pieces, const NsCall& call, Program& p)
     };
     constexpr float unscale = 1.f / SCALE_P;
     for (int done = 0; done < call.steps;) {
-        const int n = by_gram(w.s, w.l, pieces) && call.steps - done >= 2 && call.two_steps ? 2 : 1;
+        const int n = by_gram(w.s, w.l) && call.steps - done >= 2 && call.two_steps ? 2 : 1;
         add(BUF_ROWS, BUF_ROWS, BUF_A, BUF_A, false, SCALE_A / (SCALE_X * SCALE_X), 0.f, 0.f, 0.f);
         polynomial(BUF_P0, n == 1);
         int q = BUF_P0;
@@ -1196,21 +1174,20 @@ constexpr int VARIANT_BLOCK[VARIANTS] = {1, 2, 4, 8};
 
 // Blocks a round has in each size, and the largest number of units along a product's columns.  Blocks of 256 are a tenth faster than those of
 // 128 where they fill whole rounds of the 256 compute units; those of 128 need half of the chip, and columns that pay for filling four slots.
-// Whole calls (us) with fewer of them straight from the caches / through LDS: 2304 x 2304 (171 blocks) 1027 / 905, bf16 516 / 396, bf16 4 of 1024 x 1024
-// (136 .. 256) 246 / 224, bf16 1792 x 1792 (105 .. 196) 318 / 283; but 9 of 640 x 640 (135, 20 units) 276 / 306, bf16 6 of 768 x 768 (126,
-// 12 units) 185 / 196.  Straight from the caches 64 reads half of what 32 does, and takes as long for a block as there are columns for its four
+// Whole calls (us) with fewer of them straight from the caches / through LDS: 2304 x 2304 (171 blocks) 1027 / 905; but 9 of 640 x 640 (135, 20
+// units) 276 / 306.  Straight from the caches 64 reads half of what 32 does, and takes as long for a block as there are columns for its four
 // waves.  Measured, 64 / 32 (us): 136 blocks of 1024 x 1024 x 2304 19.1 / 20.8, of 1024 x 1024 x 1024 12.3 / 10.2; 312 of 4 x 768 x 768 x
 // 2304 33 / 37, x 768 15.8 / 12.8; 576 of 1024 x 2304 x 1024 27 / 31.
-int variant_for(const int64_t (&blocks)[VARIANTS], const bool (&fits)[VARIANTS], int units, int pieces)
+int variant_for(const int64_t (&blocks)[VARIANTS], const bool (&fits)[VARIANTS], int units)
 {
     const int64_t whole = (blocks[STAGED_256] + 255) / 256 * 256;
     if (fits[STAGED_256] && blocks[STAGED_256] * 100 >= whole * 88) return STAGED_256;
-    if (fits[STAGED_128] && blocks[STAGED_128] >= (pieces == 2 ? units < 32 ? 200 : 128 : units < 24 ? 128 : 100)) return STAGED_128;
+    if (fits[STAGED_128] && blocks[STAGED_128] >= (units < 32 ? 200 : 128)) return STAGED_128;
     if (blocks[DIRECT_64] >= 512 || (blocks[DIRECT_64] >= 128 && units >= 48)) return DIRECT_64;
     return DIRECT_32;
 }
 
-template <int PIECES, typename TOut, bool UPDATE>
+template <typename TOut, bool UPDATE>
 hipError_t launch_round(const Jobs& jobs, unsigned blocks, int variant, hipStream_t stream)
 {
     auto staged = [&](auto kern, int slot) {
@@ -1219,22 +1196,22 @@ hipError_t launch_round(const Jobs& jobs, unsigned blocks, int variant, hipStrea
         kern<<<dim3(blocks), dim3(512), 2 * slot, stream>>>(jobs);
         return hipGetLastError();
     };
-    if (variant == STAGED_256) return staged(ns_staged_kernel<256, PIECES, TOut, UPDATE, false>, slot_bytes<256>());
-    if (variant == STAGED_128 && blocks <= 256) return staged(ns_staged_kernel<128, PIECES, TOut, UPDATE, false, 4>, 2 * slot_bytes<128>());
-    if (variant == STAGED_128) return staged(ns_staged_kernel<128, PIECES, TOut, UPDATE, false>, slot_bytes<128>());
-    if (variant == DIVIDED_128) return staged(ns_staged_kernel<128, PIECES, TOut, UPDATE, true>, slot_bytes<128>());
-    if (variant == DIRECT_64) ns_direct_kernel<2, PIECES, TOut, UPDATE><<<dim3(blocks), dim3(256), 0, stream>>>(jobs);
-    else ns_direct_kernel<1, PIECES, TOut, UPDATE><<<dim3(blocks), dim3(256), 0, stream>>>(jobs);
+    if (variant == STAGED_256) return staged(ns_staged_kernel<256, TOut, UPDATE, false>, slot_bytes<256>());
+    if (variant == STAGED_128 && blocks <= 256) return staged(ns_staged_kernel<128, TOut, UPDATE, false, 4>, 2 * slot_bytes<128>());
+    if (variant == STAGED_128) return staged(ns_staged_kernel<128, TOut, UPDATE, false>, slot_bytes<128>());
+    if (variant == DIVIDED_128) return staged(ns_staged_kernel<128, TOut, UPDATE, true>, slot_bytes<128>());
+    if (variant == DIRECT_64) ns_direct_kernel<2, TOut, UPDATE><<<dim3(blocks), dim3(256), 0, stream>>>(jobs);
+    else ns_direct_kernel<1, TOut, UPDATE><<<dim3(blocks), dim3(256), 0, stream>>>(jobs);
     return hipGetLastError();
 }
 
 // A product of a program as a job, without its buffers; blocks of each kernel for one copy (0: it does not take this shape)
-void shape_of(const NsMatrix& m, const Layout& w, const Op& op, bool last, int pieces, Job& j, int64_t (&blocks)[VARIANTS])
+void shape_of(const NsMatrix& m, const Layout& w, const Op& op, bool last, Job& j, int64_t (&blocks)[VARIANTS])
 {
     j.symmetric = !op.with_x;
     j.m32 = (int)(w.s / 32);
     j.n32 = (int)((op.with_x ? w.l : w.s) / 32);
-    j.units = (int)((op.u == BUF_ROWS ? w.l : w.s) / (pieces == 2 ? 32 : 64));
+    j.units = (int)((op.u == BUF_ROWS ? w.l : w.s) / 32);
     if (last && m.rows > m.cols) {           // the result's rows are the columns of X
         j.m32 = (int)(w.l / 32);
         j.n32 = (int)(w.s / 32);
@@ -1250,7 +1227,7 @@ constexpr int64_t PART_BYTES = 128 * 128 * 4;
 // How many of a symmetric round's blocks of 128 are divided along their columns, and into how many parts: those that leave the 256 compute
 // units, or their two places for workgroups, unequally full.  More parts cost more for the sums (who joins a block reads all of it: 64 KiB a
 // part).  Measured, whole calls (us), undivided and divided:
-//   of 128 .. 148 blocks all, in 3: 2048 x 4096 (136) 1063 / 936, bf16 2048 x 16384 (136) 1283 / 1220; 2176 x 3840 (153)
+//   of 128 .. 148 blocks all, in 3: 2048 x 4096 (136) 1063 / 936; 2176 x 3840 (153)
 //   1251 / 1254, 2560 x 4096 (210, in 2) 1459 / 1484; 1792 x 5376 (105, in 4) 982 / 994;
 //   of 256 .. 384 those past 256, in 2: two of 2048 x 8192 (272) 2607 / 2485, in 3 2508; 3000 x 6500 (300) 2952 / 2776; 8 of
 //   1024 x 4096 (288) 1543 / 1496;
@@ -1283,7 +1260,7 @@ struct Plan {
     }
 };
 
-void plan_of(const NsMatrix* mats, int count, int pieces, const NsCall& call, Plan& plan)
+void plan_of(const NsMatrix* mats, int count, const NsCall& call, Plan& plan)
 {
     int64_t blocks[112][VARIANTS] = {};
     bool fits[112][VARIANTS];
@@ -1303,8 +1280,8 @@ void plan_of(const NsMatrix* mats, int count, int pieces, const NsCall& call, Pl
                 divided[r] = fits[r][STAGED_128] && plan.divided[r].parts > 1;
             }
         for (int i = 0; i < count; ++i) {
-            const Layout w = layout_of(mats[i].rows, mats[i].cols, pieces);
-            program_of(w, pieces, call, p);
+            const Layout w = layout_of(mats[i].rows, mats[i].cols);
+            program_of(w, call, p);
             if (pass == 0) {
                 if (p.count > plan.rounds) plan.rounds = p.count;
                 continue;
@@ -1312,13 +1289,13 @@ void plan_of(const NsMatrix* mats, int count, int pieces, const NsCall& call, Pl
             for (int k = 0; k < p.count; ++k) {
                 Job j;
                 int64_t of[VARIANTS];
-                shape_of(mats[i], w, p.op[k], k + 1 == p.count, pieces, j, of);
+                shape_of(mats[i], w, p.op[k], k + 1 == p.count, j, of);
                 const int round = plan.rounds - p.count + k;      // a shorter program ends with the longest
                 if (pass == 2) {
                     if (!divided[round]) continue;
                     int chunks, rest;
                     plan.of_copy(round, of[STAGED_128], chunks, rest);
-                    if (!j.symmetric || (int64_t)chunks * rest * plan.divided[round].parts * PART_BYTES > w.s * w.l * 2 * pieces) divided[round] = false;
+                    if (!j.symmetric || (int64_t)chunks * rest * plan.divided[round].parts * PART_BYTES > w.s * w.l * 4) divided[round] = false;
                     continue;
                 }
                 if (j.units > units[round]) units[round] = j.units;
@@ -1330,14 +1307,14 @@ void plan_of(const NsMatrix* mats, int count, int pieces, const NsCall& call, Pl
         }
     }
     for (int r = 0; r < plan.rounds; ++r) {
-        const int variant = variant_for(blocks[r], fits[r], units[r], pieces);
+        const int variant = variant_for(blocks[r], fits[r], units[r]);
         plan.variant[r] = (int8_t)(divided[r] && variant != STAGED_256 ? DIVIDED_128 : variant);
     }
 }
 
 constexpr int GROUP = JOBS;       // matrices of a launch
 
-template <typename T, int PIECES, bool UPDATE>
+template <typename T, bool UPDATE>
 hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const Plan& plan, char* ws, hipStream_t stream)
 {
     Layout w[GROUP];
@@ -1349,7 +1326,7 @@ hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const 
     unsigned sums = 0, tiles = 0;
     for (int i = 0; i < count; ++i) {
         const NsMatrix& m = mats[i];
-        w[i] = layout_of(m.rows, m.cols, PIECES);
+        w[i] = layout_of(m.rows, m.cols);
         base[i] = ws;
         ws += w[i].bytes * m.copies;
         Source& s = src.m[i];
@@ -1360,7 +1337,7 @@ hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const 
         tiles += (unsigned)(s.s_tiles * (int64_t)s.l_tiles * m.copies);
     }
     ns_norm_kernel<T, UPDATE><<<dim3(sums), dim3(256), 0, stream>>>(src);
-    ns_prepare_kernel<T, PIECES, UPDATE><<<dim3(tiles), dim3(256), 0, stream>>>(src);
+    ns_prepare_kernel<T, UPDATE><<<dim3(tiles), dim3(256), 0, stream>>>(src);
     hipError_t e = hipGetLastError();
     Program p[2];                 // step by step, two steps at a time
     int known[2] = {-1, -1};
@@ -1370,9 +1347,9 @@ hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const 
         const int variant = plan.variant[round];
         unsigned first = 0;
         for (int i = 0; i < count; ++i) {
-            const int which = by_gram(w[i].s, w[i].l, PIECES);
+            const int which = by_gram(w[i].s, w[i].l);
             if (known[which] < 0) {
-                program_of(w[i], PIECES, call, p[which]);
+                program_of(w[i], call, p[which]);
                 known[which] = 1;
             }
             const int k = round - (plan.rounds - p[which].count);
@@ -1382,7 +1359,7 @@ hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const 
             const bool last = k + 1 == p[which].count;
             Job& j = jobs.job[jobs.count++];
             int64_t blocks[VARIANTS];
-            shape_of(m, w[i], op, last, PIECES, j, blocks);
+            shape_of(m, w[i], op, last, j, blocks);
             auto at = [&](int buffer) { return (_Float16*)(base[i] + w[i].at[buffer]); };
             j.copies = (int)m.copies;
             j.stride = w[i].bytes;
@@ -1412,7 +1389,7 @@ hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const 
                 first += (unsigned)((blocks[STAGED_128] + (int64_t)j.chunks * j.rest * (j.parts - 1)) * m.copies);
             } else first += (unsigned)(blocks[variant] * m.copies);
         }
-        if (jobs.count > 0) e = launch_round<PIECES, T, UPDATE>(jobs, first, variant, stream);
+        if (jobs.count > 0) e = launch_round<T, UPDATE>(jobs, first, variant, stream);
     }
     return e;
 }
@@ -1421,7 +1398,7 @@ hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const 
 int64_t thin_slabs(const NsMatrix& m)
 {
     const int64_t s = m.rows < m.cols ? m.rows : m.cols, l = m.rows < m.cols ? m.cols : m.rows;
-    return s <= THIN_S && l <= THIN_MOST ? (padded_side(l, 2) + THIN_SLAB - 1) / THIN_SLAB * m.copies : 0;
+    return s <= THIN_S && l <= THIN_MOST ? (padded_side(l) + THIN_SLAB - 1) / THIN_SLAB * m.copies : 0;
 }
 // Once the chip is full, A and P made by every workgroup cost more than launches save (against three launches a step: 64 bf16 copies of
 // 64 x 2048, 512 slabs: 190 and 200 us; 256 fp32 copies of it: 740 and 676; 512 of 64 x 4096: 3505 and 2680)
@@ -1445,7 +1422,7 @@ hipError_t run_thin(const NsMatrix* mats, int count, const NsCall& call, char* w
     unsigned sums = 0, blocks = 0;
     for (int i = 0; i < count; ++i) {
         const NsMatrix& m = mats[i];
-        const Layout w = layout_of(m.rows, m.cols, 2);
+        const Layout w = layout_of(m.rows, m.cols);
         const int64_t size = m.rows * m.cols * (int64_t)sizeof(T);
         src.m[i] = {m.in, m.S, nullptr, nullptr, (double*)(ws + w.partial_at), w.bytes, size, (int)m.rows, (int)m.cols, 0, 0, w.parts, (int)m.copies, sums, 0, nullptr, 0};
         sums += (unsigned)(w.parts * m.copies);
@@ -1521,11 +1498,7 @@ hipError_t run_small(const NsMatrix* mats, int64_t count, const NsCall& call, hi
 
 }  // namespace
 
-// Two pieces for bf16 matrices of few rows (or columns): nothing averages the roundings of a small A (1 x 7: off by 7.9e-3 with one piece),
-// and time is not products there
-static int pieces_of(int64_t rows, int64_t cols, pex_dtype dt) { return dt == PEX_F32 || rows <= 64 || cols <= 64 ? 2 : 1; }
-
-size_t ns_matrix_bytes(int64_t rows, int64_t cols, pex_dtype dt) { return (size_t)layout_of(rows, cols, pieces_of(rows, cols, dt)).bytes; }
+size_t ns_matrix_bytes(int64_t rows, int64_t cols) { return (size_t)layout_of(rows, cols).bytes; }
 
 int ns_coefficients(const pex_newton_schulz_params& p)
 {
@@ -1573,24 +1546,22 @@ hipError_t launch_newton_schulz(const NsMatrix* mats, int64_t count, pex_dtype d
         }
         thin = thin && slabs <= THIN_MOST_SLABS;
         Plan plan;
-        const int pieces = pieces_of(together[0].rows, together[0].cols, dt);      // (bf16 matrices are of one size)
-        if (!thin) plan_of(together, members, pieces, call, plan);
+        if (!thin) plan_of(together, members, call, plan);
         size_t used = 0;
         auto flush = [&]() {
             if (n == 0 || e != hipSuccess) return;
             char* ws = (char*)workspace;
             if (thin) e = update ? run_thin<float, true>(group, n, call, ws, stream)
                                  : dt == PEX_F32 ? run_thin<float, false>(group, n, call, ws, stream) : run_thin<uint16_t, false>(group, n, call, ws, stream);
-            else if (update) e = run_group<float, 2, true>(group, n, call, plan, ws, stream);
-            else if (dt == PEX_F32) e = run_group<float, 2, false>(group, n, call, plan, ws, stream);
-            else if (pieces == 2) e = run_group<uint16_t, 2, false>(group, n, call, plan, ws, stream);
-            else e = run_group<uint16_t, 1, false>(group, n, call, plan, ws, stream);
+            else if (update) e = run_group<float, true>(group, n, call, plan, ws, stream);
+            else if (dt == PEX_F32) e = run_group<float, false>(group, n, call, plan, ws, stream);
+            else e = run_group<uint16_t, false>(group, n, call, plan, ws, stream);
             n = 0;
             used = 0;
         };
         for (int i = 0; i < members && e == hipSuccess; ++i) {
             NsMatrix m = together[i];
-            const size_t each = ns_matrix_bytes(m.rows, m.cols, dt);
+            const size_t each = ns_matrix_bytes(m.rows, m.cols);
             const int64_t elem = dt == PEX_F32 ? 4 : 2;
             while (m.copies > 0 && e == hipSuccess) {
                 int64_t fit = (int64_t)((workspace_bytes - used) / each);
