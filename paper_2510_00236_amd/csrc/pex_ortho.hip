@@ -557,6 +557,9 @@ __device__ __forceinline__ double block_sum(double s)
     return t;
 }
 
+// What a matrix of this sum of squares is multiplied with.  Zeros stay zeros, where eps = 0 too.
+__device__ __forceinline__ double to_unit(double ssq, float eps) { return ssq == 0.0 ? 0.0 : (double)SCALE_X / (sqrt(ssq) + (double)eps); }
+
 // element e of a source before it is orthogonalised; an update takes the gradient into the momentum first
 template <typename T, bool UPDATE>
 __device__ __forceinline__ float taken_in(const Momentum& momentum, T* M, const float* S, int64_t e)
@@ -634,7 +637,7 @@ __global__ __launch_bounds__(256) void ns_prepare_kernel(Sources src)
     double ssq = 0.0;
     for (int p = threadIdx.x; p < m.parts; p += 256) ssq += partial[p];
     ssq = block_sum<4>(ssq);
-    const double inv = (double)SCALE_X / (sqrt(ssq) + (double)src.eps);      // (beyond fp32's range for the smallest matrices)
+    const double inv = to_unit(ssq, src.eps);      // (beyond fp32's range for the smallest matrices)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
         const int r = 4 * i + (int)(threadIdx.x >> 6);
@@ -715,7 +718,7 @@ __global__ __launch_bounds__(SMALL_WAVES * 64) void ns_small_kernel(SmallJobs jo
         ssq += (double)u[i] * u[i];
     }
     ssq = block_sum<SMALL_WAVES>(ssq);
-    const double inv = (double)SCALE_X / (sqrt(ssq) + (double)jobs.eps);
+    const double inv = to_unit(ssq, jobs.eps);
     // entry (row, col) of an operand of cols32 times 32 columns
     auto put = [&](_Float16* to, int row, int col, int cols32, _Float16 hi, _Float16 lo) {
         _Float16* p = to + fragment_at(row >> 5, col >> 5, cols32, row >> 4 & 1, 0) + ((row & 15) + 16 * (col >> 3 & 3)) * 8 + (col & 7);
@@ -926,7 +929,7 @@ __global__ __launch_bounds__(512) void ns_thin_kernel(ThinJobs jobs)
         double ssq = 0.0;
         for (int p = threadIdx.x; p < j.parts; p += 512) ssq += partial[p];
         ssq = block_sum<8>(ssq);
-        const double inv = (double)SCALE_X / (sqrt(ssq) + (double)jobs.eps);
+        const double inv = to_unit(ssq, jobs.eps);
         const T* M = (const T*)j.M + matrix;
         const int s = tall ? j.cols : j.rows, l = tall ? j.rows : j.cols;
 #pragma unroll 8
