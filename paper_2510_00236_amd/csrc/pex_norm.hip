@@ -221,47 +221,49 @@ __global__ __launch_bounds__(THREADS) void norm_kernel(const T* X, const float* 
     }
 }
 
-// Rows too long for registers: a block per row, which it reads three times (the second and third time from the caches)
+// Rows too long for registers: a block takes a row at a time, which it reads three times (the second and third time from the caches)
 template <typename T>
-__global__ __launch_bounds__(1024) void norm_long_kernel(const T* X, const float* __restrict__ gamma, const float* __restrict__ beta, int64_t d, float eps,
-                                                         T* Y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
+__global__ __launch_bounds__(1024) void norm_long_kernel(const T* X, const float* __restrict__ gamma, const float* __restrict__ beta, int64_t rows, int64_t d,
+                                                         float eps, T* Y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
 {
     constexpr int V = Chunk<T>::N;
     __shared__ float red[2][16][1];
-    const int64_t row = blockIdx.x;
-    const T* x = X + row * d;
     int slot = 0;
-    float s[1] = {0.f};
-    for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V) {
-        const uint4_t u = load_chunk(x, j, d);
+    const float inv = 1.f / (float)d;
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T* x = X + row * d;
+        float s[1] = {0.f};
+        for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V) {
+            const uint4_t u = load_chunk(x, j, d);
 #pragma unroll
-        for (int e = 0; e < V; ++e) s[0] += value_of<T>(u, e);
-    }
-    row_sum<1024, 1024, 1>(s, red, slot);
-    const float inv = 1.f / (float)d, mu = s[0] * inv;
-    s[0] = 0.f;
-    for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V) {
-        const uint4_t u = load_chunk(x, j, d);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            const float t = j + e < d ? value_of<T>(u, e) - mu : 0.f;
-            s[0] = fmaf(t, t, s[0]);
+            for (int e = 0; e < V; ++e) s[0] += value_of<T>(u, e);
         }
-    }
-    row_sum<1024, 1024, 1>(s, red, slot);
-    const float rstd = 1.f / sqrtf(s[0] * inv + eps);
-    for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V) {
-        const uint4_t u = load_chunk(x, j, d);
-        float ga[V], be[V], y[V];
-        load_param(gamma, j, d, 1.f, ga);
-        load_param(beta, j, d, 0.f, be);
+        row_sum<1024, 1024, 1>(s, red, slot);
+        const float mu = s[0] * inv;
+        s[0] = 0.f;
+        for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V) {
+            const uint4_t u = load_chunk(x, j, d);
 #pragma unroll
-        for (int e = 0; e < V; ++e) y[e] = fmaf((value_of<T>(u, e) - mu) * rstd, ga[e], be[e]);
-        store_chunk(Y + row * d, j, d, y);
-    }
-    if (threadIdx.x == 0) {
-        if (mean_out) mean_out[row] = mu;
-        if (rstd_out) rstd_out[row] = rstd;
+            for (int e = 0; e < V; ++e) {
+                const float t = j + e < d ? value_of<T>(u, e) - mu : 0.f;
+                s[0] = fmaf(t, t, s[0]);
+            }
+        }
+        row_sum<1024, 1024, 1>(s, red, slot);
+        const float rstd = 1.f / sqrtf(s[0] * inv + eps);
+        for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V) {
+            const uint4_t u = load_chunk(x, j, d);
+            float ga[V], be[V], y[V];
+            load_param(gamma, j, d, 1.f, ga);
+            load_param(beta, j, d, 0.f, be);
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = fmaf((value_of<T>(u, e) - mu) * rstd, ga[e], be[e]);
+            store_chunk(Y + row * d, j, d, y);
+        }
+        if (threadIdx.x == 0) {
+            if (mean_out) mean_out[row] = mu;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
     }
 }
 
@@ -382,36 +384,37 @@ __global__ __launch_bounds__(THREADS, LANES == 64 && N <= 2 ? 4 : 2) void norm_g
     }
 }
 
-// Rows too long for registers: the input cotangents, a block per row
+// Rows too long for registers: the input cotangents, a row of a block at a time
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_grad_long_kernel(const T* G, const T* X, const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                              const float* __restrict__ gamma, int64_t d, T* dX)
+                                                              const float* __restrict__ gamma, int64_t rows, int64_t d, T* dX)
 {
     constexpr int V = Chunk<T>::N;
     __shared__ float red[2][16][2];
-    const int64_t row = blockIdx.x;
-    const T *g = G + row * d, *x = X + row * d;
-    const float mu = mean[row], r = rstd[row];
     int slot = 0;
-    float s[2] = {0.f, 0.f};
-    auto each = [&](int64_t j, auto f) {
-        const uint4_t ug = load_chunk(g, j, d), ux = load_chunk(x, j, d);
-        float ga[V];
-        load_param(gamma, j, d, 1.f, ga);
+    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
+        const T *g = G + row * d, *x = X + row * d;
+        const float mu = mean[row], r = rstd[row];
+        float s[2] = {0.f, 0.f};
+        auto each = [&](int64_t j, auto f) {
+            const uint4_t ug = load_chunk(g, j, d), ux = load_chunk(x, j, d);
+            float ga[V];
+            load_param(gamma, j, d, 1.f, ga);
 #pragma unroll
-        for (int e = 0; e < V; ++e) f(e, value_of<T>(ug, e) * ga[e], j + e < d ? (value_of<T>(ux, e) - mu) * r : 0.f);
-    };
-    for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V)
-        each(j, [&](int, float w, float xh) {
-            s[0] += w;
-            s[1] = fmaf(w, xh, s[1]);
-        });
-    row_sum<1024, 1024, 2>(s, red, slot);
-    const float c1 = s[0] / (float)d, c2 = s[1] / (float)d;
-    for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V) {
-        float y[V];
-        each(j, [&](int e, float w, float xh) { y[e] = r * (w - fmaf(xh, c2, c1)); });
-        store_chunk(dX + row * d, j, d, y);
+            for (int e = 0; e < V; ++e) f(e, value_of<T>(ug, e) * ga[e], j + e < d ? (value_of<T>(ux, e) - mu) * r : 0.f);
+        };
+        for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V)
+            each(j, [&](int, float w, float xh) {
+                s[0] += w;
+                s[1] = fmaf(w, xh, s[1]);
+            });
+        row_sum<1024, 1024, 2>(s, red, slot);
+        const float c1 = s[0] / (float)d, c2 = s[1] / (float)d;
+        for (int64_t j = (int64_t)threadIdx.x * V; j < d; j += 1024 * V) {
+            float y[V];
+            each(j, [&](int e, float w, float xh) { y[e] = r * (w - fmaf(xh, c2, c1)); });
+            store_chunk(dX + row * d, j, d, y);
+        }
     }
 }
 
@@ -475,6 +478,7 @@ bool with_shape(int64_t d, F&& go)
 }
 
 constexpr int64_t NORM_BLOCKS = 2048;       // eight blocks of 256 per compute unit: what is resident at once
+constexpr int64_t LONG_BLOCKS = (int64_t)1 << 20;       // of 1024: a launch holds fewer than 2^32 threads
 
 template <typename T>
 hipError_t norm_typed(const T* X, const float* gamma, const float* beta, int64_t rows, int64_t d, float eps, T* Y, float* mean, float* rstd, hipStream_t stream)
@@ -484,7 +488,7 @@ hipError_t norm_typed(const T* X, const float* gamma, const float* beta, int64_t
         const int64_t need = (rows + TH / L - 1) / (TH / L), most = NORM_BLOCKS * 256 / TH;
         norm_kernel<T, L, TH, decltype(n)::value><<<dim3((unsigned)(need < most ? need : most)), dim3(TH), 0, stream>>>(X, gamma, beta, rows, (int)d, eps, Y, mean, rstd);
     });
-    if (!fits) norm_long_kernel<T><<<dim3((unsigned)rows), dim3(1024), 0, stream>>>(X, gamma, beta, d, eps, Y, mean, rstd);
+    if (!fits) norm_long_kernel<T><<<dim3((unsigned)(rows < LONG_BLOCKS ? rows : LONG_BLOCKS)), dim3(1024), 0, stream>>>(X, gamma, beta, rows, d, eps, Y, mean, rstd);
     return hipGetLastError();
 }
 
@@ -506,7 +510,7 @@ hipError_t norm_grad_typed(const T* G, const T* X, const float* mean, const floa
         const dim3 grid((unsigned)((d + cols - 1) / cols), (unsigned)(parts < 65535 ? parts : 65535));
         norm_grad_columns_kernel<T><<<grid, dim3(256), 0, stream>>>(G, X, mean, rstd, rows, d, parts, plan.ranges, plan.per_range, partial_s, partial_o);
     }
-    norm_grad_long_kernel<T><<<dim3((unsigned)(B * rows)), dim3(1024), 0, stream>>>(G, X, mean, rstd, gamma, d, dX);
+    norm_grad_long_kernel<T><<<dim3((unsigned)(B * rows < LONG_BLOCKS ? B * rows : LONG_BLOCKS)), dim3(1024), 0, stream>>>(G, X, mean, rstd, gamma, B * rows, d, dX);
     return hipGetLastError();
 }
 

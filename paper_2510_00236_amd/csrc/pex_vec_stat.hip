@@ -150,9 +150,9 @@ __device__ __forceinline__ void finalize_wide(const float* __restrict__ partial,
 
 __global__ __launch_bounds__(CW * RW) void vec_finalize_wide_kernel(const float* __restrict__ partial, int B, int nrange, int64_t d,
                                                                float* __restrict__ s_id, float* __restrict__ s_sq,
-                                                               float* __restrict__ s_sign)
+                                                               float* __restrict__ s_sign, unsigned first)
 {
-    finalize_wide(partial, B, nrange, d, s_id, s_sq, s_sign, blockIdx.x);
+    finalize_wide(partial, B, nrange, d, s_id, s_sq, s_sign, first + blockIdx.x);
 }
 
 // Narrow blocks, for long chains over few columns: a block is 4 column lanes of VEC columns x EL example lanes x RL range lanes
@@ -379,13 +379,19 @@ bool wide_second_pass(int64_t B, int64_t d, const VecPlan& plan)
     return chain < 3 + (narrow > 256 ? (narrow - 256) / (plan.nrange == 1 ? 300 : 450) : 0);
 }
 
+constexpr int64_t MOST_BLOCKS = (int64_t)1 << 23;       // of 256: a launch holds fewer than 2^32 threads.  Narrow blocks, for d < 2^27 (no chain has 16400 steps), stay below
+
 // four columns a lane (short rows of odd length: more blocks; B=3000 d=77 22 against 27 us)
 bool in_quads(int64_t d) { return d % 4 == 0 || d >= 512; }
 
 hipError_t finalize_one(int64_t B, int64_t d, const VecPlan& plan, const float* partial, float* s_id, float* s_sq, float* s_sign, hipStream_t stream)
 {
     if (wide_second_pass(B, d, plan)) {
-        vec_finalize_wide_kernel<<<dim3((unsigned)((d + CW - 1) / CW)), dim3(CW * RW), 0, stream>>>(partial, (int)B, plan.nrange, d, s_id, s_sq, s_sign);
+        const int64_t blocks = (d + CW - 1) / CW;
+        for (int64_t first = 0; first < blocks; first += MOST_BLOCKS) {
+            const int64_t n = blocks - first < MOST_BLOCKS ? blocks - first : MOST_BLOCKS;
+            vec_finalize_wide_kernel<<<dim3((unsigned)n), dim3(CW * RW), 0, stream>>>(partial, (int)B, plan.nrange, d, s_id, s_sq, s_sign, (unsigned)first);
+        }
         return hipGetLastError();
     }
     // example lanes for the batch, the rest of the block to the ranges
@@ -477,7 +483,8 @@ hipError_t launch_vec_finalize_pair(int64_t B, int64_t d, int nrange, const floa
     const float* partial[2] = {partial0, partial1};
     const VecSums* out[2] = {&out0, &out1};
     const bool on_wide = wide_second_pass(B, d, plan);
-    if (!on_wide && !in_quads(d)) {
+    const int64_t each = on_wide ? (d + CW - 1) / CW : (d + 15) / 16;
+    if ((!on_wide && !in_quads(d)) || 2 * each > MOST_BLOCKS) {
         for (int k = 0; k < 2; ++k) {
             if (!out[k]->s_id && !out[k]->s_sq && !out[k]->s_sign) continue;
             const hipError_t e = finalize_one(B, d, plan, partial[k], out[k]->s_id, out[k]->s_sq, out[k]->s_sign, stream);
@@ -486,11 +493,10 @@ hipError_t launch_vec_finalize_pair(int64_t B, int64_t d, int nrange, const floa
         return hipSuccess;
     }
     VecBatch v{};
-    const unsigned each = (unsigned)(on_wide ? (d + CW - 1) / CW : (d + 15) / 16);
     for (int k = 0; k < 2; ++k) {
         if (!out[k]->s_id && !out[k]->s_sq && !out[k]->s_sign) continue;
         const int m = v.count++;
-        v.first[m] = each * (unsigned)m;
+        v.first[m] = (unsigned)(each * m);
         v.partial[m] = (float*)partial[k];
         v.s_id[m] = out[k]->s_id;
         v.s_sq[m] = out[k]->s_sq;
@@ -498,7 +504,7 @@ hipError_t launch_vec_finalize_pair(int64_t B, int64_t d, int nrange, const floa
         v.d[m] = d;
         v.nrange[m] = nrange;
     }
-    const dim3 grid(each * (unsigned)v.count), block(256);
+    const dim3 grid((unsigned)(each * v.count)), block(256);
     if (on_wide) vec_finalize_wide_batch_kernel<<<grid, block, 0, stream>>>(v, (int)B);
     else if (B > 16) vec_finalize_batch_kernel<64, 1><<<grid, block, 0, stream>>>(v, (int)B);
     else if (B > 4) vec_finalize_batch_kernel<16, 4><<<grid, block, 0, stream>>>(v, (int)B);
