@@ -1487,7 +1487,7 @@ hipError_t run_small(const NsMatrix* mats, int64_t count, const NsCall& call, hi
         if (!is_small(m)) continue;
         for (int64_t done = 0; done < m.copies;) {
             const int64_t n = m.copies - done < (1 << 20) ? m.copies - done : 1 << 20, skip = done * m.rows * m.cols;
-            if (jobs.count == SMALL_JOBS || blocks + (uint64_t)n > (1u << 30)) {
+            if (jobs.count == SMALL_JOBS || blocks + (uint64_t)n > (1u << 22)) {        // (of 512: a launch holds fewer than 2^32 threads)
                 const hipError_t e = flush();
                 if (e != hipSuccess) return e;
             }
