@@ -480,7 +480,8 @@ pex_status pex_layer_norm_grad(const void *G, const void *X, const float *mean, 
  *   bf16 matrices is rounded to bf16 once.  The norm is summed in fp64.  Entries of X below 2^-36 vanish: a matrix whose norm is far below
  *   eps comes out as zeros.
  *   workspace       pex_orthogonalize_workspace_bytes(...) bytes, 16-byte aligned; one matrix's (the query for count = 1) is enough, the
- *                   matrices then go through it one after the other: the same bits.  (How products are divided, and with it the
+ *                   matrices then go through it one after the other: the same bits.  Matrices of at most 16384 entries, their sides
+ *                   rounded up to multiples of 64, stay in a compute unit's memory: 256 bytes, however many they are.  (How products are divided, and with it the
  *                   last bits, goes by the sizes and number of the matrices of a call.)
  * rows, cols < 2^20, rows * cols < 2^31, count >= 1, 1 <= steps <= 32, eps >= 0 (PEX_ERR_SHAPE).  PEX_ERR_PHI: coefficients under which a
  * singular value of a step could leave [0, 4] or a step could scale one by more than 31.  Any element's address is good enough for M and O.
@@ -502,8 +503,8 @@ pex_status pex_orthogonalize(const void *M, void *O, int64_t count, int64_t rows
  *     PEX_MUON_SCALE_NONE 1,  PEX_MUON_SCALE_SHAPE sqrt(max(1, cols / rows)) (rows = din, cols = dout),
  *     PEX_MUON_SCALE_RMS  0.2 * sqrt(max(rows, cols)) (entries of the update of about 0.2, as those of Adam)
  *   tensors: host array; theta, m, S fp32 device [rows, cols] each, any float's address.
- *   workspace: pex_muon_step_workspace_bytes(...) bytes, 16-byte aligned; what the largest tensor alone needs is enough, the tensors then
- *   go through it in turn: the same bits.
+ *   workspace: pex_muon_step_workspace_bytes(...) bytes, 16-byte aligned: what the 24 tensors need that are taken at a time, in the order of
+ *   the array; what the largest tensor alone needs is enough, the tensors then go through it in turn: the same bits.
  * 0 <= momentum < 1 (PEX_ERR_SHAPE), PEX_ERR_PHI for an unknown scaling; otherwise as pex_orthogonalize, checked for every tensor before
  * anything is launched.
  */

@@ -1580,6 +1580,8 @@ static bool ns_shape_ok(int64_t rows, int64_t cols)
     return rows >= 1 && cols >= 1 && rows < side && cols < side && rows * cols < ((int64_t)1 << 31);
 }
 
+static constexpr int MUON_CHUNK = 24;        // tensors taken at a time, so that nothing is allocated: as many as share their launches
+
 static pex_status check_ns_params(const pex_newton_schulz_params& p)
 {
     if (p.steps < 1 || p.steps > 32 || !(p.eps >= 0.f) || std::isinf(p.eps)) return PEX_ERR_SHAPE;
@@ -1589,7 +1591,7 @@ static pex_status check_ns_params(const pex_newton_schulz_params& p)
 size_t pex_orthogonalize_workspace_bytes(int64_t count, int64_t rows, int64_t cols, pex_dtype dt)
 {
     if (count < 1 || count >= ((int64_t)1 << 31) || !ns_shape_ok(rows, cols) || (dt != PEX_F32 && dt != PEX_BF16)) return 0;
-    return (size_t)count * ns_matrix_bytes(rows, cols);
+    return ns_copies_bytes(count, rows, cols);
 }
 
 pex_status pex_orthogonalize(const void* M, void* O, int64_t count, int64_t rows, int64_t cols, pex_dtype dt, const pex_newton_schulz_params* p,
@@ -1611,10 +1613,12 @@ pex_status pex_orthogonalize(const void* M, void* O, int64_t count, int64_t rows
 size_t pex_muon_step_workspace_bytes(const pex_muon_tensor* tensors, int32_t count)
 {
     if (!tensors || count < 1) return 0;
-    size_t need = 0;
+    size_t need = 0, together = 0;
     for (int k = 0; k < count; ++k) {
         if (!ns_shape_ok(tensors[k].rows, tensors[k].cols)) return 0;
-        need += ns_matrix_bytes(tensors[k].rows, tensors[k].cols);
+        if (k % MUON_CHUNK == 0) together = 0;
+        together += ns_matrix_bytes(tensors[k].rows, tensors[k].cols);
+        if (together > need) need = together;
     }
     return need;
 }
@@ -1639,11 +1643,9 @@ pex_status pex_muon_step(const pex_muon_tensor* tensors, int32_t count, const pe
     if (!workspace || workspace_bytes < least) return PEX_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 15u) return PEX_ERR_ALIGN;
     const NsCall call = {p->ns.a, p->ns.b, p->ns.c, p->ns.eps, p->ns.steps, ns_coefficients(p->ns) == 2, p->momentum, (1.f - p->momentum) * p->grad_scale, p->weight_decay, p->nesterov};
-    // (a few at a time, so that nothing is allocated: as many as share their launches)
-    constexpr int CHUNK = 24;
-    for (int at = 0; at < count; at += CHUNK) {
-        NsMatrix m[CHUNK];
-        const int n = count - at < CHUNK ? count - at : CHUNK;
+    for (int at = 0; at < count; at += MUON_CHUNK) {
+        NsMatrix m[MUON_CHUNK];
+        const int n = count - at < MUON_CHUNK ? count - at : MUON_CHUNK;
         for (int k = 0; k < n; ++k) {
             const pex_muon_tensor& t = tensors[at + k];
             const double side = (double)(t.rows > t.cols ? t.rows : t.cols);

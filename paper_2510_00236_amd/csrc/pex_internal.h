@@ -216,7 +216,8 @@ struct NsCall {
     float beta, gain, decay;         // update: gain = (1 - beta) * grad_scale
     int nesterov;
 };
-size_t ns_matrix_bytes(int64_t rows, int64_t cols);            // workspace of one matrix, a multiple of 256
+size_t ns_matrix_bytes(int64_t rows, int64_t cols);                        // workspace of one matrix, a multiple of 256
+size_t ns_copies_bytes(int64_t count, int64_t rows, int64_t cols);         // of several of one size
 // 0: the iterates could leave the range of the kernels' number formats; 2: nor does what two steps multiply them with, 1 otherwise
 int ns_coefficients(const pex_newton_schulz_params& p);
 hipError_t launch_newton_schulz(const NsMatrix* mats, int64_t count, pex_dtype dt, bool update, const NsCall& call, void* workspace, size_t workspace_bytes,

@@ -1457,7 +1457,7 @@ hipError_t run_thin(const NsMatrix* mats, int count, const NsCall& call, char* w
     return e;
 }
 
-bool is_small(const NsMatrix& m) { return padded(m.rows, 64) * padded(m.cols, 64) <= SMALL_MOST; }
+bool is_small(int64_t rows, int64_t cols) { return padded(rows, 64) * padded(cols, 64) <= SMALL_MOST; }
 
 template <typename T, bool UPDATE>
 hipError_t run_small(const NsMatrix* mats, int64_t count, const NsCall& call, hipStream_t stream)
@@ -1484,7 +1484,7 @@ hipError_t run_small(const NsMatrix* mats, int64_t count, const NsCall& call, hi
     jobs.decay = call.decay;
     for (int64_t i = 0; i < count; ++i) {
         const NsMatrix& m = mats[i];
-        if (!is_small(m)) continue;
+        if (!is_small(m.rows, m.cols)) continue;
         for (int64_t done = 0; done < m.copies;) {
             const int64_t n = m.copies - done < (1 << 20) ? m.copies - done : 1 << 20, skip = done * m.rows * m.cols;
             if (jobs.count == SMALL_JOBS || blocks + (uint64_t)n > (1u << 22)) {        // (of 512: a launch holds fewer than 2^32 threads)
@@ -1501,7 +1501,9 @@ hipError_t run_small(const NsMatrix* mats, int64_t count, const NsCall& call, hi
 
 }  // namespace
 
-size_t ns_matrix_bytes(int64_t rows, int64_t cols) { return (size_t)layout_of(rows, cols).bytes; }
+// (small ones use none, but a query is never 0)
+size_t ns_matrix_bytes(int64_t rows, int64_t cols) { return is_small(rows, cols) ? 256 : (size_t)layout_of(rows, cols).bytes; }
+size_t ns_copies_bytes(int64_t count, int64_t rows, int64_t cols) { return is_small(rows, cols) ? 256 : (size_t)count * (size_t)layout_of(rows, cols).bytes; }
 
 int ns_coefficients(const pex_newton_schulz_params& p)
 {
@@ -1539,7 +1541,7 @@ hipError_t launch_newton_schulz(const NsMatrix* mats, int64_t count, pex_dtype d
         NsMatrix together[GROUP], group[GROUP];
         int members = 0, n = 0;
         for (; begin < count && members < GROUP; ++begin)
-            if (!is_small(mats[begin])) together[members++] = mats[begin];
+            if (!is_small(mats[begin].rows, mats[begin].cols)) together[members++] = mats[begin];
         if (members == 0) break;
         int64_t slabs = 0;
         bool thin = true;            // all of them: among others they share the others' launches
