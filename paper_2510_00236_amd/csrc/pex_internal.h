@@ -220,6 +220,19 @@ size_t ns_matrix_bytes(int64_t rows, int64_t cols);                        // wo
 size_t ns_copies_bytes(int64_t count, int64_t rows, int64_t cols);         // of several of one size
 // 0: the iterates could leave the range of the kernels' number formats; 2: nor does what two steps multiply them with, 1 otherwise
 int ns_coefficients(const pex_newton_schulz_params& p);
+// How matrices that go together are carried out
+constexpr int NS_GROUP = 24, NS_ROUNDS = 112;       // 32 steps: 16 times 7 products, or 32 times 3
+enum : int8_t { NS_NONE = -1, NS_DIRECT_32, NS_DIRECT_64, NS_STAGED_128, NS_STAGED_256, NS_DIVIDED_128 };
+struct NsPlan {
+    bool thin;                       // all on the kernels of thin matrices; otherwise product by product:
+    int rounds;
+    struct Round {
+        int8_t kernel[NS_GROUP];
+        int copies, divided, parts;  // of the products on blocks of 128: matrices (at most eight), blocks that are divided, into how many parts
+        int64_t blocks;              // blocks
+    } round[NS_ROUNDS];
+};
+void plan_newton_schulz(const NsMatrix* mats, int count, const NsCall& call, NsPlan& plan);
 hipError_t launch_newton_schulz(const NsMatrix* mats, int64_t count, pex_dtype dt, bool update, const NsCall& call, void* workspace, size_t workspace_bytes,
                                 hipStream_t stream);
 

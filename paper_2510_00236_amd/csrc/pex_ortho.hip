@@ -1094,6 +1094,8 @@ int64_t padded_side(int64_t n)
 }
 
 constexpr int64_t MOST_PARTS = 1024;
+constexpr int GROUP = NS_GROUP;       // matrices of a launch
+static_assert(GROUP <= JOBS && GROUP <= THIN_JOBS);
 
 // Where the buffers of one matrix lie, from the start of its part of the workspace: X by rows, twice by columns; symmetric ones
 enum : int { BUF_ROWS, BUF_COLS0, BUF_COLS1, BUF_A, BUF_P0, BUF_P1, BUF_R, BUF_COUNT };
@@ -1132,7 +1134,7 @@ struct Op {
 };
 struct Program {
     int count;
-    Op op[112];               // 32 steps: 16 times 7, or 32 times 3
+    Op op[NS_ROUNDS];
 };
 // Step by step: A = X X^T, P = a I + b A + c A^2, X = P X.  Or two steps at a time: with W = b A + c A^2, P = a I + W, the A of P X is P A P,
 // all of them polynomials of one matrix, which commute and whose products are symmetric:
@@ -1171,24 +1173,21 @@ void program_of(const Layout& w, const NsCall& call, Program& p)
     }
 }
 
-// Which kernel takes a round of products
-enum : int { DIRECT_32, DIRECT_64, STAGED_128, STAGED_256, VARIANTS, DIVIDED_128 = VARIANTS };
+// Which kernel takes a product
+enum : int { DIRECT_32 = NS_DIRECT_32, DIRECT_64, STAGED_128, STAGED_256, VARIANTS, DIVIDED_128 = VARIANTS };
+static_assert(DIRECT_64 == NS_DIRECT_64 && STAGED_256 == NS_STAGED_256 && DIVIDED_128 == NS_DIVIDED_128);
 constexpr int VARIANT_BLOCK[VARIANTS] = {1, 2, 4, 8};
 
-// Blocks a round has in each size, and the largest number of units along a product's columns.  Blocks of 256 are a tenth faster than those of
-// 128 where they fill whole rounds of the 256 compute units; those of 128 need half of the chip, and columns that pay for filling four slots.
-// Whole calls (us) with fewer of them straight from the caches / through LDS: 2304 x 2304 (171 blocks) 1027 / 905; but 9 of 640 x 640 (135, 20
-// units) 276 / 306.  Straight from the caches 64 reads half of what 32 does, and takes as long for a block as there are columns for its four
-// waves.  Measured, 64 / 32 (us): 136 blocks of 1024 x 1024 x 2304 19.1 / 20.8, of 1024 x 1024 x 1024 12.3 / 10.2; 312 of 4 x 768 x 768 x
-// 2304 33 / 37, x 768 15.8 / 12.8; 576 of 1024 x 2304 x 1024 27 / 31.
-int variant_for(const int64_t (&blocks)[VARIANTS], const bool (&fits)[VARIANTS], int units)
-{
-    const int64_t whole = (blocks[STAGED_256] + 255) / 256 * 256;
-    if (fits[STAGED_256] && blocks[STAGED_256] * 100 >= whole * 88) return STAGED_256;
-    if (fits[STAGED_128] && blocks[STAGED_128] >= (units < 32 ? 200 : 128)) return STAGED_128;
-    if (blocks[DIRECT_64] >= 512 || (blocks[DIRECT_64] >= 128 && units >= 48)) return DIRECT_64;
-    return DIRECT_32;
-}
+// By the blocks that the products of a round have in each size, and the largest number of units along a product's columns.  Blocks of 256 are a
+// tenth faster than those of 128 where they fill whole rounds of the 256 compute units; those of 128 need half of the chip, and columns
+// that pay for filling four slots.  Whole calls (us) with fewer of them straight from the caches / through LDS: 2304 x 2304 (171 blocks)
+// 1027 / 905; but 9 of 640 x 640 (135, 20 units) 276 / 306.
+bool enough_256(int64_t blocks) { return blocks * 100 >= (blocks + 255) / 256 * 256 * 88; }
+bool enough_128(int64_t blocks, int units) { return blocks >= (units < 32 ? 200 : 128); }
+// Straight from the caches 64 reads half of what 32 does, and takes as long for a block as there are columns for its four waves.  Measured,
+// 64 / 32 (us): 136 blocks of 1024 x 1024 x 2304 19.1 / 20.8, of 1024 x 1024 x 1024 12.3 / 10.2; 312 of 4 x 768 x 768 x 2304 33 / 37,
+// x 768 15.8 / 12.8; 576 of 1024 x 2304 x 1024 27 / 31.
+int direct_for(int64_t blocks_64, int units) { return blocks_64 >= 512 || (blocks_64 >= 128 && units >= 48) ? DIRECT_64 : DIRECT_32; }
 
 template <typename TOut, bool UPDATE>
 hipError_t launch_round(const Jobs& jobs, unsigned blocks, int variant, hipStream_t stream)
@@ -1246,79 +1245,98 @@ Divided divided_for(int64_t blocks, int units)
     return {(int)rest, (int)(room < most ? room : most)};
 }
 
-// The kernel of every round: all matrices of a launch as if there were workspace for them (their results do not depend on it)
-struct Plan {
-    int rounds;
-    int8_t variant[112];
-    Divided divided[112];
-    int64_t blocks[112];      // of 128
-    int copies;
-    // of a copy's blocks: chunks (some on every XCD, the divided ones last), divided ones of a chunk
-    void of_copy(int round, int64_t mine, int& chunks, int& rest) const
-    {
-        chunks = copies >= 8 || divided[round].blocks == blocks[round] ? 1 : 8 / copies;
-        if (chunks > mine) chunks = (int)mine;
-        rest = (int)((divided[round].blocks * mine + blocks[round] * chunks - 1) / (blocks[round] * chunks));
-        if (rest > mine / chunks) rest = (int)(mine / chunks);
-    }
-};
-
-void plan_of(const NsMatrix* mats, int count, const NsCall& call, Plan& plan)
+// of a copy's blocks that are divided: chunks (some on every XCD, the divided ones last), divided ones of a chunk
+void of_copy(const NsPlan::Round& round, int64_t mine, int& chunks, int& rest)
 {
-    int64_t blocks[112][VARIANTS] = {};
-    bool fits[112][VARIANTS];
-    int units[112] = {};
-    bool divided[112] = {};
-    for (auto& f : fits)
-        for (bool& x : f) x = true;
-    Program p;
-    plan.rounds = 0;
-    int64_t copies = 0;
-    for (int i = 0; i < count; ++i) copies += mats[i].copies;
-    plan.copies = copies < 8 ? (int)copies : 8;
-    for (int pass = 0; pass < 3; ++pass) {
-        if (pass == 2)
-            for (int r = 0; r < plan.rounds; ++r) {
-                plan.divided[r] = divided_for(plan.blocks[r] = blocks[r][STAGED_128], units[r]);
-                divided[r] = fits[r][STAGED_128] && plan.divided[r].parts > 1;
-            }
-        for (int i = 0; i < count; ++i) {
-            const Layout w = layout_of(mats[i].rows, mats[i].cols);
-            program_of(w, call, p);
-            if (pass == 0) {
-                if (p.count > plan.rounds) plan.rounds = p.count;
-                continue;
-            }
-            for (int k = 0; k < p.count; ++k) {
-                Job j;
-                int64_t of[VARIANTS];
-                shape_of(mats[i], w, p.op[k], k + 1 == p.count, j, of);
-                const int round = plan.rounds - p.count + k;      // a shorter program ends with the longest
-                if (pass == 2) {
-                    if (!divided[round]) continue;
-                    int chunks, rest;
-                    plan.of_copy(round, of[STAGED_128], chunks, rest);
-                    if (!j.symmetric || (int64_t)chunks * rest * plan.divided[round].parts * PART_BYTES > w.s * w.l * 4) divided[round] = false;
-                    continue;
-                }
-                if (j.units > units[round]) units[round] = j.units;
-                for (int v = 0; v < VARIANTS; ++v) {
-                    blocks[round][v] += of[v] * mats[i].copies;
-                    if (of[v] == 0) fits[round][v] = false;
-                }
-            }
-        }
+    chunks = round.copies >= 8 || round.divided == round.blocks ? 1 : 8 / round.copies;
+    if (chunks > mine) chunks = (int)mine;
+    rest = (int)((round.divided * mine + round.blocks * chunks - 1) / (round.blocks * chunks));
+    if (rest > mine / chunks) rest = (int)(mine / chunks);
+}
+
+// The kernels of all rounds of `count` matrices that go together, as if there were workspace for all of them (their results do not depend on
+// it).  Sides that are no multiple of 256, or 128, stand in the way of nobody but their own product: of a round, the products that blocks
+// of 256 take go there if these are enough, of the others those that blocks of 128 take, the rest straight from the caches, a launch
+// each.  Whole calls (us), all of a round on what every one of them takes / divided: 2048 x 8192 and 8192 x 2048 beside 2048 x 320 3860 /
+// 2676, beside 640 x 640 2987 / 2741; 2304 x 2304 beside 2304 x 320 1283 / 1008; five GPT-2 blocks beside 768 x 320 1882 / 1733.  Blocks of 128
+// pay for another launch from 6144 units of columns on, of all of them: 8 of 1024 x 1024 (288 blocks of 32) beside 1024 x 320 834 / 766,
+// but 12 of 768 x 768 (252 of 24) beside 768 x 320 586 / 589, 4 of 1024 x 1024 (144 of 32) beside 1024 x 320 500 / 523.
+void plan_rounds(const NsMatrix* mats, int count, const NsCall& call, NsPlan& plan)
+{
+    Program p[2];                 // step by step, two steps at a time
+    int known[2] = {-1, -1}, which[GROUP];
+    Layout w[GROUP];
+    for (int i = 0; i < count; ++i) {
+        w[i] = layout_of(mats[i].rows, mats[i].cols);
+        which[i] = by_gram(w[i].s, w[i].l);
+        if (known[which[i]] < 0) program_of(w[i], call, p[which[i]]);
+        known[which[i]] = 1;
+        if (p[which[i]].count > plan.rounds) plan.rounds = p[which[i]].count;
     }
     for (int r = 0; r < plan.rounds; ++r) {
-        const int variant = variant_for(blocks[r], fits[r], units[r]);
-        plan.variant[r] = (int8_t)(divided[r] && variant != STAGED_256 ? DIVIDED_128 : variant);
+        NsPlan::Round& round = plan.round[r];
+        round = {};
+        int64_t of[GROUP][VARIANTS];
+        Job j[GROUP];
+        bool open[GROUP];         // no kernel yet
+        for (int i = 0; i < count; ++i) {
+            const Program& mine = p[which[i]];
+            const int k = r - (plan.rounds - mine.count);       // a shorter program ends with the longest
+            round.kernel[i] = NS_NONE;
+            open[i] = k >= 0;
+            if (open[i]) shape_of(mats[i], w[i], mine.op[k], k + 1 == mine.count, j[i], of[i]);
+        }
+        int64_t blocks, copies, work;
+        int units;
+        bool all;                 // nobody is left
+        auto totals = [&](int variant) {
+            blocks = copies = work = units = 0;
+            all = true;
+            for (int i = 0; i < count; ++i) {
+                if (!open[i]) continue;
+                if (of[i][variant] == 0) {
+                    all = false;
+                    continue;
+                }
+                blocks += of[i][variant] * mats[i].copies;
+                copies += mats[i].copies;
+                work += of[i][variant] * mats[i].copies * j[i].units;
+                if (j[i].units > units) units = j[i].units;
+            }
+        };
+        auto take = [&](int variant, int as) {
+            for (int i = 0; i < count; ++i)
+                if (open[i] && of[i][variant] > 0) {
+                    round.kernel[i] = (int8_t)as;
+                    open[i] = false;
+                }
+        };
+        totals(STAGED_256);
+        if (blocks > 0 && enough_256(blocks)) take(STAGED_256, STAGED_256);
+        totals(STAGED_128);
+        if (enough_128(blocks, units) && (all || work >= 6144)) {
+            const Divided d = divided_for(blocks, units);
+            round.blocks = blocks;
+            round.divided = d.blocks;
+            round.parts = d.parts;
+            round.copies = copies < 8 ? (int)copies : 8;
+            bool divided = d.parts > 1;
+            for (int i = 0; i < count && divided; ++i)
+                if (open[i] && of[i][STAGED_128] > 0) {
+                    int chunks, rest;
+                    of_copy(round, of[i][STAGED_128], chunks, rest);
+                    divided = j[i].symmetric && (int64_t)chunks * rest * d.parts * PART_BYTES <= w[i].s * w[i].l * 4;
+                }
+            take(STAGED_128, divided ? DIVIDED_128 : STAGED_128);
+        }
+        totals(DIRECT_64);        // (every side is a multiple of 64)
+        take(DIRECT_64, direct_for(blocks, units));
     }
 }
 
-constexpr int GROUP = JOBS;       // matrices of a launch
-
+// `planned`: the places of the matrices in the plan
 template <typename T, bool UPDATE>
-hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const Plan& plan, char* ws, hipStream_t stream)
+hipError_t run_group(const NsMatrix* mats, const int* planned, int count, const NsCall& call, const NsPlan& plan, char* ws, hipStream_t stream)
 {
     Layout w[GROUP];
     char* base[GROUP];
@@ -1344,19 +1362,20 @@ hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const 
     hipError_t e = hipGetLastError();
     Program p[2];                 // step by step, two steps at a time
     int known[2] = {-1, -1};
-    for (int round = 0; round < plan.rounds && e == hipSuccess; ++round) {
+    for (int r = 0; r < plan.rounds * (DIVIDED_128 + 1) && e == hipSuccess; ++r) {
+        const int variant = r % (DIVIDED_128 + 1);
+        const NsPlan::Round& round = plan.round[r / (DIVIDED_128 + 1)];
         Jobs jobs{};
         jobs.decay = call.decay;
-        const int variant = plan.variant[round];
         unsigned first = 0;
         for (int i = 0; i < count; ++i) {
+            if (round.kernel[planned[i]] != variant) continue;
             const int which = by_gram(w[i].s, w[i].l);
             if (known[which] < 0) {
                 program_of(w[i], call, p[which]);
                 known[which] = 1;
             }
-            const int k = round - (plan.rounds - p[which].count);
-            if (k < 0) continue;
+            const int k = r / (DIVIDED_128 + 1) - (plan.rounds - p[which].count);
             const Op& op = p[which].op[k];
             const NsMatrix& m = mats[i];
             const bool last = k + 1 == p[which].count;
@@ -1384,8 +1403,8 @@ hipError_t run_group(const NsMatrix* mats, int count, const NsCall& call, const 
             }
             j.first = first;
             if (variant == DIVIDED_128) {
-                plan.of_copy(round, blocks[STAGED_128], j.chunks, j.rest);
-                j.share = (j.units + plan.divided[round].parts - 1) / plan.divided[round].parts;
+                of_copy(round, blocks[STAGED_128], j.chunks, j.rest);
+                j.share = (j.units + round.parts - 1) / round.parts;
                 j.parts = (j.units + j.share - 1) / j.share;
                 j.shares = (float4_t*)at(op.idle);
                 j.arrived = (unsigned*)(base[i] + w[i].arrived_at);
@@ -1529,6 +1548,21 @@ int ns_coefficients(const pex_newton_schulz_params& p)
     return largest * largest <= 60.0 ? 2 : 1;     // the product of two P's stays in P's range
 }
 
+// (thin matrices among others share the others' launches: a launch of their own for each round that goes through LDS costs no more than theirs
+// would, GPT-2's blocks or 2048 x 8192 and 8192 x 2048 beside one)
+void plan_newton_schulz(const NsMatrix* mats, int count, const NsCall& call, NsPlan& plan)
+{
+    int64_t slabs = 0;
+    plan.thin = true;
+    for (int i = 0; i < count; ++i) {
+        plan.thin = plan.thin && thin_slabs(mats[i]) > 0;
+        slabs += thin_slabs(mats[i]);
+    }
+    plan.thin = plan.thin && slabs <= THIN_MOST_SLABS;
+    plan.rounds = 0;
+    if (!plan.thin) plan_rounds(mats, count, call, plan);
+}
+
 // Small matrices in a launch of their own; the others go together, GROUP of them at a time, while there is workspace for them, copies of
 // one divided if need be
 hipError_t launch_newton_schulz(const NsMatrix* mats, int64_t count, pex_dtype dt, bool update, const NsCall& call, void* workspace, size_t workspace_bytes,
@@ -1543,24 +1577,18 @@ hipError_t launch_newton_schulz(const NsMatrix* mats, int64_t count, pex_dtype d
         for (; begin < count && members < GROUP; ++begin)
             if (!is_small(mats[begin].rows, mats[begin].cols)) together[members++] = mats[begin];
         if (members == 0) break;
-        int64_t slabs = 0;
-        bool thin = true;            // all of them: among others they share the others' launches
-        for (int i = 0; i < members; ++i) {
-            thin = thin && thin_slabs(together[i]) > 0;
-            slabs += thin_slabs(together[i]);
-        }
-        thin = thin && slabs <= THIN_MOST_SLABS;
-        Plan plan;
-        if (!thin) plan_of(together, members, call, plan);
+        NsPlan plan;
+        plan_newton_schulz(together, members, call, plan);
+        int planned[GROUP];
         size_t used = 0;
         auto flush = [&]() {
             if (n == 0 || e != hipSuccess) return;
             char* ws = (char*)workspace;
-            if (thin) e = update ? run_thin<float, true>(group, n, call, ws, stream)
+            if (plan.thin) e = update ? run_thin<float, true>(group, n, call, ws, stream)
                                  : dt == PEX_F32 ? run_thin<float, false>(group, n, call, ws, stream) : run_thin<uint16_t, false>(group, n, call, ws, stream);
-            else if (update) e = run_group<float, true>(group, n, call, plan, ws, stream);
-            else if (dt == PEX_F32) e = run_group<float, false>(group, n, call, plan, ws, stream);
-            else e = run_group<uint16_t, false>(group, n, call, plan, ws, stream);
+            else if (update) e = run_group<float, true>(group, planned, n, call, plan, ws, stream);
+            else if (dt == PEX_F32) e = run_group<float, false>(group, planned, n, call, plan, ws, stream);
+            else e = run_group<uint16_t, false>(group, planned, n, call, plan, ws, stream);
             n = 0;
             used = 0;
         };
@@ -1577,6 +1605,7 @@ hipError_t launch_newton_schulz(const NsMatrix* mats, int64_t count, pex_dtype d
                 }
                 NsMatrix part = m;
                 if (part.copies > fit) part.copies = fit;
+                planned[n] = i;
                 group[n++] = part;
                 used += each * (size_t)part.copies;
                 m.copies -= part.copies;
