@@ -403,6 +403,19 @@ def _workspace(query, args, like, workspace, stream=None):
     return workspace, _dev(workspace, "workspace"), workspace.numel()
 
 
+def _new(stream, *shape, dtype, device, zeros=False):
+    """A tensor that a call makes for its result, allocated (and cleared) under the stream the kernels run on: memory of another stream's
+    pool may still be in use there.  It is not handed out again before what the current stream does with it is done."""
+    make = _torch.zeros if zeros else _torch.empty
+    if stream is None:
+        return make(*shape, dtype=dtype, device=device)
+    with _torch.cuda.stream(stream):
+        t = make(*shape, dtype=dtype, device=device)
+    if t.is_cuda:
+        t.record_stream(_torch.cuda.current_stream(t.device))
+    return t
+
+
 def _check_workspace_size(workspace, nbytes):
     if workspace is not None and workspace.numel() < nbytes:
         raise ValueError(f"workspace holds {workspace.numel()} bytes, the call needs {nbytes}")
@@ -429,7 +442,7 @@ def pex_stat(X, G, phi, S=None, workspace=None, stream=None):
     dt = _dtype_code(X)
     code = PHI.get(phi, phi)
     if S is None:
-        S = _torch.empty(din, dout, dtype=_torch.float32, device=X.device)
+        S = _new(stream, din, dout, dtype=_torch.float32, device=X.device)
     query, qargs = pex_stat_workspace_bytes, (B, T, din, dout, dt, code)
     ws, wptr, wbytes = _workspace(query, qargs, X, workspace, stream)
     _invoke_ws(query, qargs, ws, lib().pex_stat, _dev(X, "X"), _dev(G, "G"), B, T, din, dout, dt, code, _f32(S, "S", shape=(din, dout)), wptr, wbytes,
@@ -467,7 +480,7 @@ def pex_stat_multi(X, G, want, out=None, workspace=None, stream=None):
         if mask & bit:
             S = (out or {}).get(name)
             if S is None:
-                S = _torch.empty(din, dout, dtype=_torch.float32, device=X.device)
+                S = _new(stream, din, dout, dtype=_torch.float32, device=X.device)
             res[name] = S
             ptrs.append(_f32(S, name, shape=(din, dout)))
         else:
@@ -500,7 +513,7 @@ def pex_vec_stat(A, C=None, want=("identity", "square", "sign"), out=None, works
         if mask & bit:
             s = (out or {}).get(name)
             if s is None:
-                s = _torch.empty(d, dtype=_torch.float32, device=A.device)
+                s = _new(stream, d, dtype=_torch.float32, device=A.device)
             res[name] = s
             ptrs.append(_f32(s, name, numel=d))
         else:
@@ -550,7 +563,7 @@ def pex_stat_pair_batch(layers, workspace=None, stream=None):
         for name in ("identity", "square"):
             S = (out or {}).get(name)
             if S is None:
-                S = _torch.empty(din, dout, dtype=_F32, device=X.device)
+                S = _new(stream, din, dout, dtype=_F32, device=X.device)
             r[name] = S
             rows.append(_f32(S, name, shape=(din, dout)))
         rows += (din, dout)
@@ -595,7 +608,7 @@ def pex_vec_stat_batch(items, want=("identity", "square", "sign"), workspace=Non
             if mask & bit:
                 s = (out or {}).get(name)
                 if s is None:
-                    s = _torch.empty(d, dtype=_F32, device=A.device)
+                    s = _new(stream, d, dtype=_F32, device=A.device)
                 r[name] = s
                 rows.append(_f32(s, name, numel=d))
             else:
@@ -634,7 +647,7 @@ def pex_example_norms(X, G, N=None, workspace=None, stream=None):
     B, T, din, dout = _shapes(X, G)
     dt = _dtype_code(X)
     if N is None:
-        N = _torch.empty(B, dtype=_torch.float32, device=X.device)
+        N = _new(stream, B, dtype=_torch.float32, device=X.device)
     query, qargs = pex_example_norms_workspace_bytes, (B, T, din, dout, dt)
     ws, wptr, wbytes = _workspace(query, qargs, X, workspace, stream)
     _invoke_ws(query, qargs, ws, lib().pex_example_norms, _dev(X, "X"), _dev(G, "G"), B, T, din, dout, dt, _f32(N, "N", numel=B), wptr, wbytes,
@@ -653,7 +666,7 @@ def pex_weighted_sum(X, G, w, S=None, workspace=None, stream=None):
     B, T, din, dout = _shapes(X, G)
     dt = _dtype_code(X)
     if S is None:
-        S = _torch.empty(din, dout, dtype=_torch.float32, device=X.device)
+        S = _new(stream, din, dout, dtype=_torch.float32, device=X.device)
     query, qargs = pex_weighted_sum_workspace_bytes, (B, T, din, dout, dt)
     ws, wptr, wbytes = _workspace(query, qargs, X, workspace, stream)
     _invoke_ws(query, qargs, ws, lib().pex_weighted_sum, _dev(X, "X"), _dev(G, "G"), _f32(w, "w", numel=B), B, T, din, dout, dt, _f32(S, "S", shape=(din, dout)), wptr,
@@ -674,7 +687,7 @@ def pex_clip_weights(N, max_norm, w=None, stream=None):
         raise ValueError("N must be [layers, B] or [B]")
     nlayers, B = (1, N.shape[0]) if N.dim() == 1 else (int(N.shape[0]), int(N.shape[1]))
     if w is None:
-        w = _torch.empty(B, dtype=_torch.float32, device=N.device)
+        w = _new(stream, B, dtype=_torch.float32, device=N.device)
     _invoke(lib().pex_clip_weights, _f32(N, "N"), B, nlayers, float(max_norm), _f32(w, "w", numel=B), _stream(stream))
     return w
 
@@ -686,7 +699,7 @@ def pex_stat_power(X, G, alpha, S=None, workspace=None, stream=None):
     B, T, din, dout = _shapes(X, G)
     dt = _dtype_code(X)
     if S is None:
-        S = _torch.empty(din, dout, dtype=_torch.float32, device=X.device)
+        S = _new(stream, din, dout, dtype=_torch.float32, device=X.device)
     query, qargs = pex_stat_power_workspace_bytes, (B, T, din, dout, dt)
     ws, wptr, wbytes = _workspace(query, qargs, X, workspace, stream)
     _invoke_ws(query, qargs, ws, lib().pex_stat_power, _dev(X, "X"), _dev(G, "G"), B, T, din, dout, dt, float(alpha), _f32(S, "S", shape=(din, dout)), wptr,
@@ -701,7 +714,7 @@ def pex_token_norms(X, G, N_tok=None, stream=None):
     B, T, din, dout = _shapes(X, G)
     dt = _dtype_code(X)
     if N_tok is None:
-        N_tok = _torch.empty(B, T, dtype=_torch.float32, device=X.device)
+        N_tok = _new(stream, B, T, dtype=_torch.float32, device=X.device)
     _invoke(lib().pex_token_norms, _dev(X, "X"), _dev(G, "G"), B, T, din, dout, dt, _f32(N_tok, "N_tok", numel=B * T), _stream(stream))
     return N_tok
 
@@ -717,7 +730,7 @@ def pex_token_sq(X, G, S=None, workspace=None, stream=None):
     B, T, din, dout = _shapes(X, G)
     dt = _dtype_code(X)
     if S is None:
-        S = _torch.empty(din, dout, dtype=_torch.float32, device=X.device)
+        S = _new(stream, din, dout, dtype=_torch.float32, device=X.device)
     query, qargs = pex_token_sq_workspace_bytes, (B, T, din, dout, dt)
     ws, wptr, wbytes = _workspace(query, qargs, X, workspace, stream)
     _invoke_ws(query, qargs, ws, lib().pex_token_sq, _dev(X, "X"), _dev(G, "G"), B, T, din, dout, dt, _f32(S, "S", shape=(din, dout)), wptr, wbytes,
@@ -768,7 +781,7 @@ def pex_moment_track(ema_adam, ema_micro, S_id, S_sq, params: MomentParams, sums
         _bind_torch()
     n = ema_adam.numel()
     if sums is None:
-        sums = _torch.empty(2, dtype=_torch.float64, device=ema_adam.device)
+        sums = _new(stream, 2, dtype=_torch.float64, device=ema_adam.device)
     query, qargs = pex_moment_track_workspace_bytes, (n,)
     ws, wptr, wbytes = _workspace(query, qargs, ema_adam, workspace, stream)
     _invoke_ws(query, qargs, ws, lib().pex_moment_track, _f32(ema_adam, "ema_adam"), _f32(ema_micro, "ema_micro", n), _f32(S_id, "S_id", n),
@@ -801,7 +814,7 @@ def pex_embed_stat(ids, G, V, want, out=None, workspace=None, stream=None):
         if mask & bit:
             S = (out or {}).get(name)
             if S is None:
-                S = _torch.empty(V, d, dtype=_torch.float32, device=G.device)
+                S = _new(stream, V, d, dtype=_torch.float32, device=G.device)
             res[name] = S
             ptrs.append(_f32(S, name, shape=(V, d)))
         else:
@@ -838,7 +851,7 @@ def pex_mfma_probe(operands, workgroups, iters, sink=None, stream=None):
     if operands.numel() * operands.element_size() < need:
         raise ValueError(f"operands must hold at least {need} bytes")
     if sink is None:
-        sink = _torch.empty(pex_mfma_probe_sink_floats(workgroups), dtype=_torch.float32, device=operands.device)
+        sink = _new(stream, pex_mfma_probe_sink_floats(workgroups), dtype=_torch.float32, device=operands.device)
     flop = ctypes.c_double(0.0)
     _invoke(lib().pex_mfma_probe, _dev(operands, "operands"), int(workgroups), int(iters), _f32(sink, "sink"), ctypes.byref(flop),
                                 _stream(stream))
@@ -855,7 +868,7 @@ def pex_sum_squares(x, acc=None, accumulate=False, workspace=None, stream=None):
         _bind_torch()
     n = x.numel()
     if acc is None:
-        acc = _torch.zeros(1, dtype=_torch.float64, device=x.device)
+        acc = _new(stream, 1, dtype=_torch.float64, device=x.device, zeros=True)
     query, qargs = pex_sum_squares_workspace_bytes, (n,)
     ws, wptr, wbytes = _workspace(query, qargs, x, workspace, stream)
     _invoke_ws(query, qargs, ws, lib().pex_sum_squares, _f32(x, "x"), n, _f64(acc, "acc", 1), int(bool(accumulate)), wptr, wbytes, _stream(stream))
@@ -909,7 +922,7 @@ def pex_adam_step(tensors, variant, params: AdamParams, sum_sq, max_norm, moment
         rows.append(n)
         sizes.append(n)
     if moments is not None and sums is None:
-        sums = _torch.empty(len(sizes), 2, dtype=_F64, device=sum_sq.device)
+        sums = _new(stream, len(sizes), 2, dtype=_F64, device=sum_sq.device)
     sums_at = _f64(sums, "sums", 2 * len(sizes)) if moments is not None else None
     keep, at = _table(rows)
     query, qargs = pex_adam_step_workspace_bytes, (sizes,)
@@ -934,7 +947,7 @@ def pex_layer_norm(X, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
         raise ValueError("expected X[..., d]")
     dt, rows, d = _dtype_code(X), X.shape[:-1], X.shape[-1]
     if out is None:
-        out = (_torch.empty_like(X), _torch.empty(rows, dtype=_F32, device=X.device), _torch.empty(rows, dtype=_F32, device=X.device))
+        out = (_new(stream, X.shape, dtype=X.dtype, device=X.device), _new(stream, rows, dtype=_F32, device=X.device), _new(stream, rows, dtype=_F32, device=X.device))
     Y, mean, rstd = out
     n = X.numel() // d if d else 0
     _invoke(lib().pex_layer_norm, _dev(X, "X"), _f32(gamma, "gamma", d) if gamma is not None else None, _f32(beta, "beta", d) if beta is not None else None,
@@ -965,7 +978,7 @@ def pex_layer_norm_grad(G, X, mean, rstd, gamma=None, want=("identity", "square"
     B, T, d = G.shape
     dt, mask = _dtype_code(G), _want_mask(want)
     if dX is None:
-        dX = _torch.empty_like(G)
+        dX = _new(stream, G.shape, dtype=G.dtype, device=G.device)
     res, ptrs = {}, []
     for p in ("scale", "offset"):
         given, r = (out or {}).get(p) or {}, {}
@@ -973,7 +986,7 @@ def pex_layer_norm_grad(G, X, mean, rstd, gamma=None, want=("identity", "square"
             if mask & bit and (offset or p == "scale"):
                 s = given.get(name)
                 if s is None:
-                    s = _torch.empty(d, dtype=_F32, device=G.device)
+                    s = _new(stream, d, dtype=_F32, device=G.device)
                 r[name] = s
                 ptrs.append(_f32(s, p + " " + name, numel=d))
             else:
@@ -1004,7 +1017,7 @@ def pex_orthogonalize(M, out=None, params: NewtonSchulzParams = None, workspace=
     dt = _dtype_code(M)
     count, rows, cols = (1, *M.shape) if M.dim() == 2 else M.shape
     if out is None:
-        out = _torch.empty_like(M)
+        out = _new(stream, M.shape, dtype=M.dtype, device=M.device)
     if params is None:
         params = NewtonSchulzParams()
     at, out_at = _dev(M, "M"), _dev(out, "out", M.dtype, shape=M.shape)
