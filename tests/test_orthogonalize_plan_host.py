@@ -66,7 +66,17 @@ def test_thin_matrices(kernels):
 
 # of tests on the GPU: the kernels that they are there for
 @pytest.mark.parametrize("matrices,steps,has", [
-    ([(2048, 3300)], 5, "4"), ([(1024, 1600, 8)], 5, "4"), ([(768, 768, 12)], 5, "2"), ([(130, 513)], 5, "0"), ([(1200, 2000, 5)], 5, "2")])
+    ([(2048, 3300)], 5, "4"), ([(1024, 1600, 8)], 5, "4"), ([(768, 768, 12)], 5, "2"), ([(130, 513)], 5, "0"), ([(1200, 2000, 5)], 5, "2"),
+    ([(2048, 8192, 1)], 5, "34"), ([(8192, 2048, 1)], 5, "34"), ([(2000, 8190, 1)], 5, "34"), ([(2048, 2048, 7)], 5, "3"), ([(5376, 5400, 1)], 5, "3"),
+    (LARGE, 5, "34"), ([(2304, 2304)], 5, "2"), ([(2048, 2048)] * 7, 5, "3")])
 def test_kernels_that_tests_reach(kernels, matrices, steps, has):
     found = kernels(matrices, steps)[1]
     assert set(has) <= set("".join(found)), found
+
+
+def test_two_steps_at_a_time_through_the_gram_matrix(kernels):
+    """Seven products two steps, three the last of an odd number"""
+    for rows, cols in ((520, 1000), (1900, 600), (1024, 1600)):
+        for steps in (1, 2, 3, 4, 6, 7):
+            assert len(kernels([(rows, cols)], steps)[1][0]) == steps // 2 * 7 + steps % 2 * 3
+    assert len(kernels([(700, 1000)], 4)[1][0]) == 12
