@@ -1585,7 +1585,7 @@ static constexpr int MUON_CHUNK = 24;        // tensors taken at a time, so that
 static pex_status check_ns_params(const pex_newton_schulz_params& p)
 {
     if (p.steps < 1 || p.steps > 32 || !(p.eps >= 0.f) || std::isinf(p.eps)) return PEX_ERR_SHAPE;
-    return ns_coefficients(p) > 0 ? PEX_OK : PEX_ERR_PHI;
+    return ns_coefficients_ok(p) ? PEX_OK : PEX_ERR_PHI;
 }
 
 size_t pex_orthogonalize_workspace_bytes(int64_t count, int64_t rows, int64_t cols, pex_dtype dt)
@@ -1606,7 +1606,7 @@ pex_status pex_orthogonalize(const void* M, void* O, int64_t count, int64_t rows
     if (!workspace || workspace_bytes < ns_matrix_bytes(rows, cols)) return PEX_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 15u) return PEX_ERR_ALIGN;
     const NsMatrix m = {const_cast<void*>(M), nullptr, O, rows, cols, count, 0.f};
-    const NsCall call = {p->a, p->b, p->c, p->eps, p->steps, ns_coefficients(*p) == 2, 0.f, 0.f, 0.f, 0};
+    const NsCall call = {p->a, p->b, p->c, p->eps, p->steps, 0.f, 0.f, 0.f, 0};
     return launch_newton_schulz(&m, 1, dt, false, call, workspace, workspace_bytes, (hipStream_t)stream) == hipSuccess ? PEX_OK : PEX_ERR_HIP;
 }
 
@@ -1642,7 +1642,8 @@ pex_status pex_muon_step(const pex_muon_tensor* tensors, int32_t count, const pe
     }
     if (!workspace || workspace_bytes < least) return PEX_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 15u) return PEX_ERR_ALIGN;
-    const NsCall call = {p->ns.a, p->ns.b, p->ns.c, p->ns.eps, p->ns.steps, ns_coefficients(p->ns) == 2, p->momentum, (1.f - p->momentum) * p->grad_scale, p->weight_decay, p->nesterov};
+    const NsCall call = {p->ns.a, p->ns.b, p->ns.c, p->ns.eps, p->ns.steps, p->momentum,
+                         (1.f - p->momentum) * p->grad_scale, p->weight_decay, p->nesterov};
     for (int at = 0; at < count; at += MUON_CHUNK) {
         NsMatrix m[MUON_CHUNK];
         const int n = count - at < MUON_CHUNK ? count - at : MUON_CHUNK;

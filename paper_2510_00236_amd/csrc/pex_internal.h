@@ -212,14 +212,13 @@ struct NsMatrix {
 struct NsCall {
     float a, b, c, eps;
     int steps;
-    bool two_steps;                  // two steps at a time may go through the Gram matrix
     float beta, gain, decay;         // update: gain = (1 - beta) * grad_scale
     int nesterov;
 };
 size_t ns_matrix_bytes(int64_t rows, int64_t cols);                        // workspace of one matrix, a multiple of 256
 size_t ns_copies_bytes(int64_t count, int64_t rows, int64_t cols);         // of several of one size
-// 0: the iterates could leave the range of the kernels' number formats; 2: nor does what two steps multiply them with, 1 otherwise
-int ns_coefficients(const pex_newton_schulz_params& p);
+// Whether the iterates, and what they are multiplied with, stay in the range of the kernels' number formats
+bool ns_coefficients_ok(const pex_newton_schulz_params& p);
 // How matrices that go together are carried out
 constexpr int NS_GROUP = 24, NS_ROUNDS = 112;       // 32 steps: 16 times 7 products, or 32 times 3
 enum : int8_t { NS_NONE = -1, NS_DIRECT_32, NS_DIRECT_64, NS_STAGED_128, NS_STAGED_256, NS_DIVIDED_128 };

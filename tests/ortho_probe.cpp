@@ -16,8 +16,7 @@ int main()
             if (scanf("%lld %lld %lld", &rows, &cols, &copies) != 3) return 1;
             m[i] = {nullptr, nullptr, nullptr, rows, cols, copies, 0.f};
         }
-        const pex_newton_schulz_params p = {a, b, c, 1e-7f, steps};
-        const pex::NsCall call = {a, b, c, 1e-7f, steps, pex::ns_coefficients(p) == 2, 0.f, 0.f, 0.f, 0};
+        const pex::NsCall call = {a, b, c, 1e-7f, steps, 0.f, 0.f, 0.f, 0};
         static pex::NsPlan plan;
         pex::plan_newton_schulz(m, count, call, plan);
         printf("%d %d", (int)plan.thin, plan.rounds);
