@@ -1560,7 +1560,7 @@ pex_status pex_layer_norm_grad(const void* G, const void* X, const float* mean, 
     if (((uintptr_t)G | (uintptr_t)X | (uintptr_t)dX) & (esz - 1)) return PEX_ERR_ALIGN;
     if (((uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)gamma | (uintptr_t)scale.s_id | (uintptr_t)scale.s_sq | (uintptr_t)scale.s_sign |
          (uintptr_t)offset.s_id | (uintptr_t)offset.s_sq | (uintptr_t)offset.s_sign) & 3u) return PEX_ERR_ALIGN;
-    if (!want) {        // rows are rows: B examples of them could be more blocks than a launch holds
+    if (!want && B >= 65536) {        // rows are rows: B examples of them could be more blocks than a launch holds
         T *= B;
         B = 1;
     }
