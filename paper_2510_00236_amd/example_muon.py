@@ -4,8 +4,9 @@
 
 The block is y = x + f(norm(x) W1) W2 with f(a) = a sigmoid(a).  A step calls, in this order (everything on the GPU, nothing synchronises with the host):
   1. pex_layer_norm, which keeps mean and 1/std of every row; the two products of the forward pass are torch's;
-  2. the products of the backward pass (torch), then pex_layer_norm_grad: the cotangents of the block's input, and S_id and S_sq of scale and
-     offset, whose per-example gradients are sums over the sequence;
+  2. the products of the backward pass (torch), then pex_layer_norm_grad: the cotangents of the norm's input (a layer before the block would
+     receive their sum with those of its output, the residual path's), and S_id and S_sq of scale and offset, whose per-example gradients
+     are sums over the sequence;
   3. pex_stat(identity) of the two matrices: the sum of their gradients over the batch;
   4. pex_muon_step of the matrices, pex_adam_step (MicroAdam, clipped by the global norm of the two vectors) of scale and offset.
 """
