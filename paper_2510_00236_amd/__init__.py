@@ -1033,31 +1033,35 @@ def pex_muon_step_workspace_bytes(shapes) -> int:
     return int(lib().pex_muon_step_workspace_bytes(at, len(shapes)))
 
 
-def _as_rows_of(t, name, S):
-    """fp32 ``t`` whose memory is a matrix of S's rows: flat, of S's shape, or of one whose leading dimensions are S's rows.  (Another matrix
+def _check_rows(t, name, S):
+    """Whether the memory of ``t``, of another shape than S, is a matrix of S's rows: its leading dimensions are those rows.  (Another matrix
     of as many elements, the transpose of S's shape above all, would be updated along the wrong directions.)"""
-    if t.dim() > 1 and t.shape != S.shape:
-        rows, lead = S.shape[0], 1
-        for n in t.shape:
-            if lead == rows:
-                break
-            lead *= n
-        if lead != rows:
-            raise ValueError(f"{name} must be flat or lie as S{tuple(S.shape)} does, got {tuple(t.shape)}")
-    return _f32(t, name, S.numel())
+    rows, lead = S.shape[0], 1
+    for n in t.shape:
+        if lead == rows:
+            break
+        lead *= n
+    if lead != rows:
+        raise ValueError(f"{name} must be flat or lie as S{tuple(S.shape)} does, got {tuple(t.shape)}")
 
 
 def pex_muon_step(tensors, params: MuonParams, workspace=None, stream=None):
     """One in-place step of Muon over all weight matrices of a model: ``tensors`` are (theta, m, S) in fp32, S [din, dout] (as pex_stat
-    returns it), theta and m of the same layout (that shape, flat, or with either side divided).  A workspace for the largest is enough; with room for all of them they go together."""
+    returns it), theta and m of the same layout (that shape, flat, or with either side divided).  A workspace for the largest is enough; with
+    room for all of them they go together."""
     if _torch is None:
         _bind_torch()
     rows, shapes = [], []
     for theta, m, S in tensors:
         if S.dim() != 2:
             raise ValueError(f"expected S[din, dout], got {tuple(S.shape)}")
-        rows += (_as_rows_of(theta, "theta", S), _as_rows_of(m, "m", S), _f32(S, "S"), S.shape[0], S.shape[1])
-        shapes.append((S.shape[0], S.shape[1]))
+        shape, n = S.shape, S.numel()
+        if theta.shape != shape and theta.dim() > 1:
+            _check_rows(theta, "theta", S)
+        if m.shape != shape and m.dim() > 1:
+            _check_rows(m, "m", S)
+        rows += (_f32(theta, "theta", n), _f32(m, "m", n), _f32(S, "S"), *shape)
+        shapes.append(tuple(shape))
     if not shapes:
         raise ValueError("expected at least one tensor")
     keep, at = _table(rows)

@@ -1365,6 +1365,9 @@ hipError_t run_group(const NsMatrix* mats, const int* planned, int count, const 
     for (int r = 0; r < plan.rounds * (DIVIDED_128 + 1) && e == hipSuccess; ++r) {
         const int variant = r % (DIVIDED_128 + 1);
         const NsPlan::Round& round = plan.round[r / (DIVIDED_128 + 1)];
+        bool any = false;
+        for (int i = 0; i < count; ++i) any = any || round.kernel[planned[i]] == variant;
+        if (!any) continue;
         Jobs jobs{};
         jobs.decay = call.decay;
         unsigned first = 0;
@@ -1411,7 +1414,7 @@ hipError_t run_group(const NsMatrix* mats, const int* planned, int count, const 
                 first += (unsigned)((blocks[STAGED_128] + (int64_t)j.chunks * j.rest * (j.parts - 1)) * m.copies);
             } else first += (unsigned)(blocks[variant] * m.copies);
         }
-        if (jobs.count > 0) e = launch_round<T, UPDATE>(jobs, first, variant, stream);
+        e = launch_round<T, UPDATE>(jobs, first, variant, stream);
     }
     return e;
 }
